@@ -55,8 +55,14 @@ typedef enum {
   HELIX_ERR_WORKSPACE = 6,
   HELIX_ERR_LAUNCH = 7,
   HELIX_ERR_BAD_STRIDE = 8,
-  HELIX_ERR_SCRATCH_LIMIT = 9
+  HELIX_ERR_SCRATCH_LIMIT = 9,
+  HELIX_ERR_BAD_TYPE = 10,
+  HELIX_ERR_BAD_PROBABILITY = 11,
+  HELIX_ERR_BAD_EPSILON = 12
 } helix_status;
+
+/* Element type of the activations of the row-wise operators. */
+typedef enum { HELIX_BF16 = 0, HELIX_F16 = 1, HELIX_F32 = 2 } helix_type;
 
 /* Element strides of a logical [B, H, S, D] bf16 tensor whose D elements per row are
  * contiguous: element (b, h, s, d) lives at base + b*batch + h*head + s*row + d.  Used by
@@ -220,6 +226,70 @@ int helix_qkv_linear_bwd(const void* a, long long lda, const void* w, long long 
                          int M, int K, int N, void* stream);
 /* Bytes of scratch helix_qkv_linear_bwd needs (0 for an invalid shape).  Pure host arithmetic. */
 size_t helix_qkv_linear_bwd_workspace_bytes(int M, int K, int N);
+
+/* ---- The layer in front of and behind its attention stage (pre-attention and post-attention,
+ * Section 2.1).  Recomputation without attention (Section 4.4) runs the forward calls below a
+ * second time before their backward calls.
+ *
+ * Row-wise operators: activations are M rows (tokens) of E elements of `type` (a helix_type) in
+ * device memory, the rows contiguous, ld* elements between consecutive rows (ld* >= E, M * ld* below
+ * 2^40; HELIX_ERR_BAD_STRIDE).  Any M >= 1 and E >= 1 (E <= HELIX_NORM_MAX_COLS with a layer norm).
+ * No alignment is asked for beyond that of an element; rows that start on 16-byte boundaries are the
+ * fastest.  Parameters, their gradients and the row statistics are contiguous fp32.  Arithmetic is fp32;
+ * activations are rounded once, when they are stored.  Padding between the rows is not written.
+ *
+ * Dropout with probability p, 0 <= p < 1 (HELIX_ERR_BAD_PROBABILITY): an element is dropped with the
+ * probability p' = cut / 2^16, cut = round(p * 2^16) (at most 2^16 - 1), and multiplied by 1 / (1 - p') otherwise.
+ * Random numbers come from the counter-based generator Philox4x32-10: row i of the call and the eight columns
+ * from 8c on take the block of counter (c, first_row + i, offset mod 2^32, offset / 2^32) under the key (seed
+ * mod 2^32, seed / 2^32); column 8c + e takes the low (e even) or high (e odd) half of the block's word e / 2
+ * and stays if it is >= cut.  `rng` is DEVICE memory, 8-byte aligned, holding seed and offset, two unsigned
+ * 64-bit numbers that the kernels read when they run: a captured graph draws new numbers when the offset is
+ * changed between its replays.  The mask is a function of (seed, offset, first_row + i, column) alone and is never
+ * stored: the backward call, and a forward call that is run again, take the same rng and first_row and find
+ * the same mask, whatever the type, the strides or the number of rows of the call.  0 <= first_row, first_row + M <= 2^32
+ * (HELIX_ERR_BAD_SHAPE).  A dropped element is zero whatever its value was.  With cut == 0 rng is not read and may be NULL.
+ *
+ * helix_dropout_add_fwd: out = residual + keep * x / (1 - p').  residual NULL: out = keep * x / (1 - p').
+ * helix_dropout_add_bwd: dx = keep * dout / (1 - p').  (The residual's gradient is dout itself.) */
+int helix_dropout_add_fwd(const void* x, long long ldx, const void* residual, long long ldr, void* out, long long ldo,
+                          int M, int E, int type, float p, const unsigned long long* rng, long long first_row, void* stream);
+int helix_dropout_add_bwd(const void* dout, long long lddout, void* dx, long long lddx,
+                          int M, int E, int type, float p, const unsigned long long* rng, long long first_row, void* stream);
+
+/* Layer norm over the E elements of a row:
+ *   y = (x - mean) * rstd * gamma + beta,  rstd = 1 / sqrt(var + eps), var = mean of (x - mean)^2
+ *   gamma, beta : in,  fp32 [E];  eps finite and > 0 (HELIX_ERR_BAD_EPSILON)
+ *   mean, rstd  : out, fp32 [M], what the backward needs; either may be NULL
+ * Backward, with xh = (x - mean) * rstd and g = dy * gamma:
+ *   dx = rstd * (g - mean(g) - xh * mean(g * xh)),  dgamma = sum over rows of dy * xh,  dbeta = sum over rows of dy
+ *   dgamma, dbeta : out, fp32 [E] (overwritten, not accumulated)
+ *   workspace     : device scratch of at least helix_layer_norm_bwd_workspace_bytes(M, E) bytes, 256-byte aligned, for
+ *                   partial sums over rows that are then added in a fixed order (no atomics: every bit is reproduced). */
+#define HELIX_NORM_MAX_COLS 16384
+int helix_layer_norm_fwd(const void* x, long long ldx, const float* gamma, const float* beta, void* y, long long ldy,
+                         float* mean, float* rstd, int M, int E, int type, float eps, void* stream);
+int helix_layer_norm_bwd(const void* dy, long long lddy, const void* x, long long ldx, const float* gamma,
+                         const float* mean, const float* rstd, void* dx, long long lddx, float* dgamma, float* dbeta,
+                         void* workspace, size_t workspace_bytes, int M, int E, int type, void* stream);
+/* Bytes of scratch the two backward calls with a layer norm need (0 for an invalid shape).  Pure host arithmetic. */
+size_t helix_layer_norm_bwd_workspace_bytes(int M, int E);
+
+/* Dropout, residual sum and layer norm in one pass, as they follow the output projection of attention:
+ *   s = residual + keep * x / (1 - p'),  y = layer norm of s
+ *   s : out, the new residual stream.  The statistics and y are those of the fp32 sum before it is rounded to s.
+ * Backward:
+ *   dresidual = ds + (gradient of the layer norm of s for dy),  dx = keep * dresidual / (1 - p')
+ *   ds : in, what reaches s directly (the residual connection behind it), or NULL for none */
+int helix_dropout_add_layer_norm_fwd(const void* x, long long ldx, const void* residual, long long ldr, void* s, long long lds,
+                                     const float* gamma, const float* beta, void* y, long long ldy, float* mean, float* rstd,
+                                     int M, int E, int type, float p, const unsigned long long* rng, long long first_row,
+                                     float eps, void* stream);
+int helix_dropout_add_layer_norm_bwd(const void* dy, long long lddy, const void* ds, long long ldds, const void* s, long long lds,
+                                     const float* gamma, const float* mean, const float* rstd, void* dx, long long lddx,
+                                     void* dresidual, long long lddr, float* dgamma, float* dbeta,
+                                     void* workspace, size_t workspace_bytes, int M, int E, int type,
+                                     float p, const unsigned long long* rng, long long first_row, void* stream);
 
 /* Whether `strides` (NULL: contiguous) is acceptable for a [B, H, S, D] view: HELIX_OK,
  * HELIX_ERR_BAD_STRIDE, or the shape errors of the other calls.  Pure host arithmetic: the

@@ -17,6 +17,8 @@ EXPORTS = ("helix_attn_fwd", "helix_attn_bwd", "helix_attn_bwd_static", "helix_a
            "helix_attn_check_strides", "helix_qkv_linear_fwd", "helix_qkv_linear_bwd", "helix_qkv_linear_bwd_workspace_bytes",
            "helix_attn_bwd_workspace_bytes",
            "helix_attn_bwd_preprocess", "helix_attn_bwd_delta_head", "helix_attn_bwd_dkdv", "helix_attn_bwd_dq",
+           "helix_dropout_add_fwd", "helix_dropout_add_bwd", "helix_layer_norm_fwd", "helix_layer_norm_bwd", "helix_layer_norm_bwd_workspace_bytes",
+           "helix_dropout_add_layer_norm_fwd", "helix_dropout_add_layer_norm_bwd",
            "helix_attn_device_info", "helix_mfma_probe", "helix_mfma_mix_probe", "helix_status_string", "helix_attn_version")
 HELIX_OK = 0
 _lib = None
@@ -61,6 +63,17 @@ def lib() -> ctypes.CDLL:
         L.helix_qkv_linear_bwd_workspace_bytes.restype = sz
         L.helix_qkv_linear_fwd.restype = i
         L.helix_qkv_linear_bwd.restype = i
+        L.helix_dropout_add_fwd.argtypes = [vp, ll, vp, ll, vp, ll, i, i, i, f, vp, ll, vp]
+        L.helix_dropout_add_bwd.argtypes = [vp, ll, vp, ll, i, i, i, f, vp, ll, vp]
+        L.helix_layer_norm_fwd.argtypes = [vp, ll, fp, fp, vp, ll, fp, fp, i, i, i, f, vp]
+        L.helix_layer_norm_bwd.argtypes = [vp, ll, vp, ll, fp, fp, fp, vp, ll, fp, fp, vp, sz, i, i, i, vp]
+        L.helix_layer_norm_bwd_workspace_bytes.argtypes = [i, i]
+        L.helix_layer_norm_bwd_workspace_bytes.restype = sz
+        L.helix_dropout_add_layer_norm_fwd.argtypes = [vp, ll, vp, ll, vp, ll, fp, fp, vp, ll, fp, fp, i, i, i, f, vp, ll, f, vp]
+        L.helix_dropout_add_layer_norm_bwd.argtypes = [vp, ll, vp, ll, vp, ll, fp, fp, fp, vp, ll, vp, ll, fp, fp, vp, sz, i, i, i, f, vp, ll, vp]
+        for name in ("helix_dropout_add_fwd", "helix_dropout_add_bwd", "helix_layer_norm_fwd", "helix_layer_norm_bwd",
+                     "helix_dropout_add_layer_norm_fwd", "helix_dropout_add_layer_norm_bwd"):
+            getattr(L, name).restype = i
         L.helix_attn_bwd_workspace_bytes.argtypes = [i, i, i, i]
         L.helix_attn_bwd_workspace_bytes.restype = sz
         L.helix_attn_bwd_preprocess.argtypes = [vp, vp, fp, vp, i, i, i, i, vp]
@@ -306,3 +319,126 @@ def helix_qkv_linear_bwd(a, w, dqkv, da, dw, workspace=None, stream=None):
     _raise(lib().helix_qkv_linear_bwd(pa, lda, pw, ldw, pg, ldg, pda, ldda, pdw, lddw, _ptr(workspace),
                                       0 if workspace is None else workspace.numel(), M, K, N, _stream(stream)),
            "helix_qkv_linear_bwd")
+
+
+# ---------------------------------------------------------------- row-wise operators
+_TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
+
+
+def _here(stream, *tensors):
+    """Every tensor (None: left out) lives on the current device, whose stream the call goes to."""
+    device = torch.cuda.current_device() if _device is None else _device()
+    if stream is not None and stream.device_index != device:
+        raise ValueError(f"stream: belongs to device {stream.device_index}, the current one is {device}")
+    for t in tensors:
+        if t is not None and t.get_device() != device:
+            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{device}")
+
+
+def _activation(name, t, like):
+    """(pointer, elements between rows) of a 2-D device matrix with the type and shape of `like` whose rows are contiguous."""
+    if not t.is_cuda or t.dtype is not like.dtype or t.dim() != 2 or t.shape != like.shape:
+        raise ValueError(f"{name}: need a CUDA {like.dtype} matrix of shape {tuple(like.shape)}")
+    rows, cols = t.shape
+    ld, one = t.stride()
+    if one != 1 and cols > 1:
+        raise ValueError(f"{name}: need contiguous rows")
+    return t.data_ptr(), ld if rows > 1 else max(ld, cols)   # a single row has no next one
+
+
+def _rows(name, t):
+    """(rows, columns, type) of an activation."""
+    if t.dim() != 2 or t.dtype not in _TYPES:
+        raise ValueError(f"{name}: need a matrix of bfloat16, float16 or float32")
+    return t.shape[0], t.shape[1], _TYPES[t.dtype]
+
+
+def _generator(rng):
+    """rng: None, or a CUDA int64 tensor with the two elements seed and offset."""
+    if rng is None:
+        return None
+    if rng.dtype is not torch.int64 or not rng.is_cuda or not rng.is_contiguous() or rng.numel() != 2:
+        raise ValueError("rng: need a contiguous CUDA int64 tensor of two elements, seed and offset")
+    return rng.data_ptr()
+
+
+def _workspace(workspace):
+    if workspace.dtype is not torch.uint8 or not workspace.is_cuda or not workspace.is_contiguous():
+        raise ValueError("workspace: need a contiguous CUDA uint8 tensor")
+    return workspace.data_ptr(), workspace.numel()
+
+
+def _statistics(M, E, **tensors):
+    """Pointers of fp32 vectors: mean and rstd have M elements, the others E; None stays None."""
+    for name, t in tensors.items():
+        if t is not None:
+            _check_f32(name, t, (M if name in ("mean", "rstd") else E,))
+    return [_ptr(t) for t in tensors.values()]
+
+
+def helix_dropout_add_fwd(x, residual, out, p, rng, first_row=0, stream=None):
+    """out[M,E] <- residual + dropout(x); residual None: dropout(x).  rng: CUDA int64 tensor [seed, offset] (None where p == 0);
+    row i takes the random numbers of row first_row + i."""
+    M, E, kind = _rows("x", x)
+    (px, ldx), (po, ldo) = _activation("x", x, x), _activation("out", out, x)
+    pr, ldr = (None, 0) if residual is None else _activation("residual", residual, x)
+    pg = _generator(rng)
+    _here(stream, x, residual, out, rng)
+    _raise(lib().helix_dropout_add_fwd(px, ldx, pr, ldr, po, ldo, M, E, kind, float(p), pg, int(first_row), _stream(stream)), "helix_dropout_add_fwd")
+
+
+def helix_dropout_add_bwd(dout, dx, p, rng, first_row=0, stream=None):
+    """dx[M,E] <- gradient of the dropped-out branch; the residual's gradient is dout itself."""
+    M, E, kind = _rows("dout", dout)
+    (pg, ldg), (px, ldx) = _activation("dout", dout, dout), _activation("dx", dx, dout)
+    pr = _generator(rng)
+    _here(stream, dout, dx, rng)
+    _raise(lib().helix_dropout_add_bwd(pg, ldg, px, ldx, M, E, kind, float(p), pr, int(first_row), _stream(stream)), "helix_dropout_add_bwd")
+
+
+def helix_layer_norm_fwd(x, gamma, beta, y, mean, rstd, eps=1e-5, stream=None):
+    """y[M,E], mean[M], rstd[M] <- layer norm of the rows of x; gamma, beta: fp32 [E].  mean and rstd may be None."""
+    M, E, kind = _rows("x", x)
+    (px, ldx), (py, ldy) = _activation("x", x, x), _activation("y", y, x)
+    pg, pb, pm, pr = _statistics(M, E, gamma=gamma, beta=beta, mean=mean, rstd=rstd)
+    _here(stream, x, gamma, beta, y, mean, rstd)
+    _raise(lib().helix_layer_norm_fwd(px, ldx, pg, pb, py, ldy, pm, pr, M, E, kind, float(eps), _stream(stream)), "helix_layer_norm_fwd")
+
+
+def helix_layer_norm_bwd_workspace_bytes(M, E) -> int:
+    return int(lib().helix_layer_norm_bwd_workspace_bytes(M, E))
+
+
+def helix_layer_norm_bwd(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, workspace, stream=None):
+    """dx[M,E], dgamma[E], dbeta[E] <- gradients of helix_layer_norm_fwd; workspace: uint8 CUDA tensor of
+    helix_layer_norm_bwd_workspace_bytes(M, E) bytes."""
+    M, E, kind = _rows("x", x)
+    (pdy, lddy), (px, ldx), (pdx, lddx) = _activation("dy", dy, x), _activation("x", x, x), _activation("dx", dx, x)
+    pg, pm, pr, pdg, pdb = _statistics(M, E, gamma=gamma, mean=mean, rstd=rstd, dgamma=dgamma, dbeta=dbeta)
+    pw, nw = _workspace(workspace)
+    _here(stream, dy, x, gamma, mean, rstd, dx, dgamma, dbeta, workspace)
+    _raise(lib().helix_layer_norm_bwd(pdy, lddy, px, ldx, pg, pm, pr, pdx, lddx, pdg, pdb, pw, nw, M, E, kind, _stream(stream)), "helix_layer_norm_bwd")
+
+
+def helix_dropout_add_layer_norm_fwd(x, residual, s, gamma, beta, y, mean, rstd, p, rng, eps=1e-5, first_row=0, stream=None):
+    """s <- residual + dropout(x), y, mean, rstd <- layer norm of s (see helix_dropout_add_fwd and helix_layer_norm_fwd)."""
+    M, E, kind = _rows("x", x)
+    (px, ldx), (pr, ldr), (ps, lds), (py, ldy) = (_activation(n, t, x) for n, t in (("x", x), ("residual", residual), ("s", s), ("y", y)))
+    pg, pb, pm, pd = _statistics(M, E, gamma=gamma, beta=beta, mean=mean, rstd=rstd)
+    pn = _generator(rng)
+    _here(stream, x, residual, s, gamma, beta, y, mean, rstd, rng)
+    _raise(lib().helix_dropout_add_layer_norm_fwd(px, ldx, pr, ldr, ps, lds, pg, pb, py, ldy, pm, pd, M, E, kind, float(p), pn, int(first_row),
+                                                  float(eps), _stream(stream)), "helix_dropout_add_layer_norm_fwd")
+
+
+def helix_dropout_add_layer_norm_bwd(dy, ds, s, gamma, mean, rstd, dx, dresidual, dgamma, dbeta, workspace, p, rng, first_row=0, stream=None):
+    """dresidual <- ds + gradient of the layer norm of s, dx <- its dropped-out share, dgamma, dbeta.  ds may be None."""
+    M, E, kind = _rows("s", s)
+    (pdy, lddy), (ps, lds), (pdx, lddx), (pdr, lddr) = (_activation(n, t, s) for n, t in (("dy", dy), ("s", s), ("dx", dx), ("dresidual", dresidual)))
+    pds, ldds = (None, 0) if ds is None else _activation("ds", ds, s)
+    pg, pm, pr, pdg, pdb = _statistics(M, E, gamma=gamma, mean=mean, rstd=rstd, dgamma=dgamma, dbeta=dbeta)
+    pw, nw = _workspace(workspace)
+    pn = _generator(rng)
+    _here(stream, dy, ds, s, gamma, mean, rstd, dx, dresidual, dgamma, dbeta, workspace, rng)
+    _raise(lib().helix_dropout_add_layer_norm_bwd(pdy, lddy, pds, ldds, ps, lds, pg, pm, pr, pdx, lddx, pdr, lddr, pdg, pdb, pw, nw, M, E, kind, float(p),
+                                                  pn, int(first_row), _stream(stream)), "helix_dropout_add_layer_norm_bwd")

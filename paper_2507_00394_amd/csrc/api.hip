@@ -2,6 +2,7 @@
 // validation first, with no HIP call before it succeeds, then kernel launches on the
 // caller's stream.  Nothing is allocated, freed or synchronised.
 #include "../../include/helix_attn.h"
+#include "dispatch.hpp"
 #include "kernels.hpp"
 
 #include <cmath>
@@ -18,7 +19,7 @@ namespace {
 constexpr size_t kScratchBytes = HELIX_STATIC_SCRATCH_BYTES;
 static __device__ __align__(256) unsigned char scratch[kScratchBytes];
 
-constexpr int kVersion = 300;  // 0.3.0: backward stages share one statistics workspace; probes; allocation-free backward
+constexpr int kVersion = 400;  // 0.4.0: the row-wise operators around the attention stage
 
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
@@ -107,6 +108,39 @@ int check_linear(int M, int K, int N, bool need_m32, std::initializer_list<std::
     // 255 rows of a stage tile times the row pitch in bytes stays below 2^31: lane offsets of the copies fit 32 bits with room to spare
     if (ld.first < ld.second || (ld.first & 7) || ld.first > (1 << 22)) return HELIX_ERR_BAD_STRIDE;
   return HELIX_OK;
+}
+
+// Row-wise operators.  `activations`: pointer and pitch of each.
+int check_rows(int M, int E, int type, bool norm, std::initializer_list<std::pair<const void*, long long>> activations,
+               std::initializer_list<const void*> f32) {
+  if (type != HELIX_BF16 && type != HELIX_F16 && type != HELIX_F32) return HELIX_ERR_BAD_TYPE;
+  for (const auto& a : activations) if (!a.first) return HELIX_ERR_NULL_POINTER;
+  for (const void* p : f32) if (!p) return HELIX_ERR_NULL_POINTER;
+  for (const auto& a : activations) if (!aligned(a.first, type == HELIX_F32 ? 4 : 2)) return HELIX_ERR_MISALIGNED;
+  for (const void* p : f32) if (!aligned(p, 4)) return HELIX_ERR_MISALIGNED;
+  if (M < 1 || E < 1 || E > (1 << 30) || (norm && E > HELIX_NORM_MAX_COLS)) return HELIX_ERR_BAD_SHAPE;
+  for (const auto& a : activations)
+    if (a.second < E || a.second >= (1LL << 40) || (double)a.second * M >= 1099511627776.0) return HELIX_ERR_BAD_STRIDE;   // 2^40 elements
+  return HELIX_OK;
+}
+int to_dropout(float p, const unsigned long long* rng, long long first_row, int M, helix::Dropout* out) {
+  if (!(p >= 0.f && p < 1.f)) return HELIX_ERR_BAD_PROBABILITY;
+  const long cut = std::lrint((double)p * 65536.);
+  out->cut = cut > 65535 ? 65535u : (unsigned)cut;
+  out->scale = 65536.f / (float)(65536 - (int)out->cut);
+  if (out->cut && !rng) return HELIX_ERR_NULL_POINTER;
+  if (out->cut && !aligned(rng, 8)) return HELIX_ERR_MISALIGNED;
+  if (first_row < 0 || first_row > (1LL << 32) - M) return HELIX_ERR_BAD_SHAPE;
+  out->rng = rng;
+  out->first_row = (unsigned)first_row;
+  return HELIX_OK;
+}
+int check_eps(float eps) { return std::isfinite(eps) && eps > 0.f ? HELIX_OK : HELIX_ERR_BAD_EPSILON; }
+int check_f32_or_null(const void* p) { return aligned(p, 4) ? HELIX_OK : HELIX_ERR_MISALIGNED; }
+int check_workspace(const void* p, size_t bytes, size_t need) {
+  if (!p) return HELIX_ERR_NULL_POINTER;
+  if (!aligned(p, 256)) return HELIX_ERR_MISALIGNED;
+  return bytes < need ? HELIX_ERR_WORKSPACE : HELIX_OK;
 }
 
 int launched(hipError_t e) { return e == hipSuccess ? HELIX_OK : HELIX_ERR_LAUNCH; }
@@ -290,6 +324,72 @@ int helix_qkv_linear_bwd(const void* a, long long lda, const void* w, long long 
   return launched(helix::launch_linear_bwd(a, lda, w, ldw, dqkv, lddqkv, da, ldda, dw, lddw, workspace, M, K, N, (hipStream_t)stream));
 }
 
+int helix_dropout_add_fwd(const void* x, long long ldx, const void* residual, long long ldr, void* out, long long ldo,
+                          int M, int E, int type, float p, const unsigned long long* rng, long long first_row, void* stream) {
+  if (residual) HELIX_TRY(check_rows(M, E, type, false, {{x, ldx}, {residual, ldr}, {out, ldo}}, {}));
+  else HELIX_TRY(check_rows(M, E, type, false, {{x, ldx}, {out, ldo}}, {}));
+  helix::Dropout drop;
+  HELIX_TRY(to_dropout(p, rng, first_row, M, &drop));
+  return launched(helix::launch_dropout_add(x, ldx, residual, ldr, out, ldo, M, E, (helix::ElementType)type, drop, (hipStream_t)stream));
+}
+
+int helix_dropout_add_bwd(const void* dout, long long lddout, void* dx, long long lddx,
+                          int M, int E, int type, float p, const unsigned long long* rng, long long first_row, void* stream) {
+  return helix_dropout_add_fwd(dout, lddout, nullptr, 0, dx, lddx, M, E, type, p, rng, first_row, stream);
+}
+
+int helix_layer_norm_fwd(const void* x, long long ldx, const float* gamma, const float* beta, void* y, long long ldy,
+                         float* mean, float* rstd, int M, int E, int type, float eps, void* stream) {
+  HELIX_TRY(check_rows(M, E, type, true, {{x, ldx}, {y, ldy}}, {gamma, beta}));
+  HELIX_TRY(check_f32_or_null(mean));
+  HELIX_TRY(check_f32_or_null(rstd));
+  HELIX_TRY(check_eps(eps));
+  const helix::NormFwd a = {x, nullptr, nullptr, y, gamma, beta, mean, rstd, ldx, 0, 0, ldy, M, E, eps, {nullptr, 0, 0, 1.f}};
+  return launched(helix::launch_norm_fwd(a, (helix::ElementType)type, (hipStream_t)stream));
+}
+
+int helix_dropout_add_layer_norm_fwd(const void* x, long long ldx, const void* residual, long long ldr, void* s, long long lds,
+                                     const float* gamma, const float* beta, void* y, long long ldy, float* mean, float* rstd,
+                                     int M, int E, int type, float p, const unsigned long long* rng, long long first_row,
+                                     float eps, void* stream) {
+  HELIX_TRY(check_rows(M, E, type, true, {{x, ldx}, {residual, ldr}, {s, lds}, {y, ldy}}, {gamma, beta}));
+  HELIX_TRY(check_f32_or_null(mean));
+  HELIX_TRY(check_f32_or_null(rstd));
+  HELIX_TRY(check_eps(eps));
+  helix::NormFwd a = {x, residual, s, y, gamma, beta, mean, rstd, ldx, ldr, lds, ldy, M, E, eps, {}};
+  HELIX_TRY(to_dropout(p, rng, first_row, M, &a.drop));
+  return launched(helix::launch_norm_fwd(a, (helix::ElementType)type, (hipStream_t)stream));
+}
+
+size_t helix_layer_norm_bwd_workspace_bytes(int M, int E) {
+  if (M < 1 || E < 1 || E > HELIX_NORM_MAX_COLS) return 0;
+  return ((size_t)helix::norm_bwd_groups(M, E) * 2 * E * sizeof(float) + 255) & ~(size_t)255;
+}
+
+int helix_layer_norm_bwd(const void* dy, long long lddy, const void* x, long long ldx, const float* gamma,
+                         const float* mean, const float* rstd, void* dx, long long lddx, float* dgamma, float* dbeta,
+                         void* workspace, size_t workspace_bytes, int M, int E, int type, void* stream) {
+  HELIX_TRY(check_rows(M, E, type, true, {{dy, lddy}, {x, ldx}, {dx, lddx}}, {gamma, mean, rstd, dgamma, dbeta}));
+  HELIX_TRY(check_workspace(workspace, workspace_bytes, helix_layer_norm_bwd_workspace_bytes(M, E)));
+  const helix::NormBwd a = {dy, nullptr, x, dx, nullptr, gamma, mean, rstd, dgamma, dbeta, static_cast<float*>(workspace),
+                            lddy, 0, ldx, lddx, 0, M, E, {nullptr, 0, 0, 1.f}};
+  return launched(helix::launch_norm_bwd(a, (helix::ElementType)type, (hipStream_t)stream));
+}
+
+int helix_dropout_add_layer_norm_bwd(const void* dy, long long lddy, const void* ds, long long ldds, const void* s, long long lds,
+                                     const float* gamma, const float* mean, const float* rstd, void* dx, long long lddx,
+                                     void* dresidual, long long lddr, float* dgamma, float* dbeta,
+                                     void* workspace, size_t workspace_bytes, int M, int E, int type,
+                                     float p, const unsigned long long* rng, long long first_row, void* stream) {
+  HELIX_TRY(check_rows(M, E, type, true, {{dy, lddy}, {s, lds}, {dx, lddx}, {dresidual, lddr}}, {gamma, mean, rstd, dgamma, dbeta}));
+  if (ds) HELIX_TRY(check_rows(M, E, type, true, {{ds, ldds}}, {}));
+  HELIX_TRY(check_workspace(workspace, workspace_bytes, helix_layer_norm_bwd_workspace_bytes(M, E)));
+  helix::NormBwd a = {dy, ds, s, dx, dresidual, gamma, mean, rstd, dgamma, dbeta, static_cast<float*>(workspace),
+                      lddy, ldds, lds, lddx, lddr, M, E, {}};
+  HELIX_TRY(to_dropout(p, rng, first_row, M, &a.drop));
+  return launched(helix::launch_norm_bwd(a, (helix::ElementType)type, (hipStream_t)stream));
+}
+
 int helix_mfma_probe(float* sink, int workgroups, int iters, int random_operands, long long* flops, void* stream) {
   if (!sink || !flops) return HELIX_ERR_NULL_POINTER;
   if (!aligned(sink, 4)) return HELIX_ERR_MISALIGNED;
@@ -328,6 +428,9 @@ const char* helix_status_string(int status) {
     case HELIX_ERR_LAUNCH: return "kernel launch failed";
     case HELIX_ERR_SCRATCH_LIMIT: return "shape too large for the built-in scratch of helix_attn_bwd_static: B*H*S must not exceed 4194304";
     case HELIX_ERR_BAD_STRIDE: return "bad strides: multiples of 8 elements, row stride at least the row length and within the index limits, dimensions nested without overlap";
+    case HELIX_ERR_BAD_TYPE: return "bad type: not one of the element types or activations";
+    case HELIX_ERR_BAD_PROBABILITY: return "bad dropout probability: must be >= 0 and < 1";
+    case HELIX_ERR_BAD_EPSILON: return "bad epsilon: must be finite and > 0";
     default: return "unknown status";
   }
 }

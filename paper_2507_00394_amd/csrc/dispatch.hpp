@@ -333,4 +333,23 @@ inline TilePair linear_gradient_tiles(int M, int K, int N, int parts) {
   return TilePair{(TileKind)best->input, (TileKind)best->weight};
 }
 
+// ---------------------------------------------------------------- layer norm's rows
+//
+// How many lanes hold a row, and how many chunks of 8 columns a lane at most: as few lanes as have it in registers, with few registers a lane.
+enum class NormRows { k16x2, k64x2, k256x1, k256x2, k512x2, k1024x2 };
+constexpr int kNormMaxCols = 16384;
+inline NormRows norm_rows(int cols) {
+  return cols <= 256 ? NormRows::k16x2 : cols <= 1024 ? NormRows::k64x2 : cols <= 2048 ? NormRows::k256x1 : cols <= 4096 ? NormRows::k256x2
+       : cols <= 8192 ? NormRows::k512x2 : NormRows::k1024x2;
+}
+inline int norm_lanes(NormRows r) { return r == NormRows::k16x2 ? 16 : r == NormRows::k64x2 ? 64 : r == NormRows::k512x2 ? 512 : r == NormRows::k1024x2 ? 1024 : 256; }
+// Workgroups of `threads` that the chip holds at once: 32 waves a compute unit.
+inline int norm_groups_at_once(int threads) { return 256 * 2048 / threads; }
+// Workgroups of the gradient.  Each leaves a slab of partial sums of dgamma and dbeta.
+inline int norm_bwd_groups(int rows, int cols) {
+  const int lanes = norm_lanes(norm_rows(cols)), threads = lanes > 256 ? lanes : 256, together = threads / lanes;
+  const long long turns = ((long long)rows + together - 1) / together;   // of a workgroup, if there were only one
+  return (int)std::min<long long>(turns, 256 * 1024 / threads);
+}
+
 }  // namespace helix

@@ -80,4 +80,36 @@ hipError_t launch_mfma_probe(float* sink, int workgroups, int iters, bool random
 // mix) or, forward_mix, 3 fma + 1 exp2.  One workgroup per compute unit (64 KB of LDS).  Same FLOP count.
 hipError_t launch_mfma_mix_probe(float* sink, int workgroups, int iters, bool forward_mix, hipStream_t stream);
 
+// Row-wise operators (rows.hip) on matrices of `rows` x `cols` elements; ld*: elements between consecutive rows.
+enum class ElementType { bf16, f16, f32 };
+// cut = round(p * 2^16), 0: nothing is dropped and `rng` (device: seed, offset) is not read; scale = 2^16 / (2^16 - cut).
+struct Dropout {
+  const unsigned long long* rng;
+  unsigned first_row, cut;
+  float scale;
+};
+struct NormFwd {   // r and s null: y is the layer norm of x; else s = r + keep * x * scale and y is the layer norm of s
+  const void *x, *r;
+  void *s, *y;
+  const float *gamma, *beta;
+  float *mean, *rstd;   // either may be null
+  long long ldx, ldr, lds, ldy;
+  int rows, cols;
+  float eps;
+  Dropout drop;
+};
+struct NormBwd {   // dr null: dx is the gradient of x; else x is the sum s, dr its gradient (ds, if not null, added) and dx = keep * scale * dr
+  const void *dy, *ds, *x;
+  void *dx, *dr;
+  const float *gamma, *mean, *rstd;
+  float *dgamma, *dbeta, *partial;   // partial: norm_bwd_groups(rows, cols) slabs of 2 * cols
+  long long lddy, ldds, ldx, lddx, lddr;
+  int rows, cols;
+  Dropout drop;
+};
+hipError_t launch_dropout_add(const void* x, long long ldx, const void* r, long long ldr, void* out, long long ldo, int rows, int cols, ElementType type,
+                              const Dropout& drop, hipStream_t stream);   // r may be null
+hipError_t launch_norm_fwd(const NormFwd& a, ElementType type, hipStream_t stream);
+hipError_t launch_norm_bwd(const NormBwd& a, ElementType type, hipStream_t stream);
+
 }  // namespace helix
