@@ -61,6 +61,9 @@ typedef enum {
   HELIX_ERR_BAD_EPSILON = 12
 } helix_status;
 
+/* Activation of the gated projections: g / (1 + e^-g), or g times the normal distribution function of g. */
+typedef enum { HELIX_SILU = 0, HELIX_GELU = 1 } helix_activation;
+
 /* Element type of the activations of the row-wise operators. */
 typedef enum { HELIX_BF16 = 0, HELIX_F16 = 1, HELIX_F32 = 2 } helix_type;
 
@@ -290,6 +293,26 @@ int helix_dropout_add_layer_norm_bwd(const void* dy, long long lddy, const void*
                                      void* dresidual, long long lddr, float* dgamma, float* dbeta,
                                      void* workspace, size_t workspace_bytes, int M, int E, int type,
                                      float p, const unsigned long long* rng, long long first_row, void* stream);
+
+/* The gated feed-forward projections: both products, the activation and their product in one kernel.
+ *   forward : [g u] = a w,  h = act(g) * u
+ *   backward: dg = dh * u * act'(g),  du = dh * act(g),  da = [dg du] w^T,  dw = a^T [dg du]
+ *   a  : bf16 [M][K];  w : bf16 [K][2F], the gate's F columns first;  h, dh : bf16 [M][F];  da : bf16 [M][K]
+ *   gu : bf16 [M][2F] or NULL.  Forward: out, [g u] for the backward.  Backward: in, what the forward wrote; NULL: the
+ *        projections are computed again from a and w (4MKF FLOPs more, and nothing to keep but a).
+ *   dw : bf16 [K][2F] (overwritten, not accumulated), summed in fp32 and rounded once
+ * activation: a helix_activation (HELIX_ERR_BAD_TYPE).  Any M >= 1; K a multiple of 128 and F of 64 (HELIX_ERR_BAD_SHAPE).  Pointers and
+ * ld* as for helix_qkv_linear_fwd: 16-byte aligned, ld* at least the row length, a multiple of 8, at most 2^22 (HELIX_ERR_BAD_STRIDE).
+ * The down projection h -> [M][K] is helix_qkv_linear_fwd / _bwd with F in the place of K.
+ * workspace: device memory of at least helix_gated_linear_bwd_workspace_bytes(M, K, F) bytes, 256-byte aligned, contents undefined
+ * afterwards: [dg du], and what helix_qkv_linear_bwd keeps there.  No atomics: every bit is reproduced. */
+int helix_gated_linear_fwd(const void* a, long long lda, const void* w, long long ldw, void* gu, long long ldgu,
+                           void* h, long long ldh, int M, int K, int F, int activation, void* stream);
+int helix_gated_linear_bwd(const void* a, long long lda, const void* w, long long ldw, const void* gu, long long ldgu,
+                           const void* dh, long long lddh, void* da, long long ldda, void* dw, long long lddw,
+                           void* workspace, size_t workspace_bytes, int M, int K, int F, int activation, void* stream);
+/* Bytes of scratch helix_gated_linear_bwd needs (0 for an invalid shape).  Pure host arithmetic. */
+size_t helix_gated_linear_bwd_workspace_bytes(int M, int K, int F);
 
 /* Whether `strides` (NULL: contiguous) is acceptable for a [B, H, S, D] view: HELIX_OK,
  * HELIX_ERR_BAD_STRIDE, or the shape errors of the other calls.  Pure host arithmetic: the

@@ -64,3 +64,33 @@ def layer_norm_bwd_ref(dy, x, gamma, mean, rstd):
     g = dy * gamma
     dx = rstd[:, None] * (g - g.mean(1, keepdims=True) - xh * (g * xh).mean(1, keepdims=True))
     return dx, (dy * xh).sum(0), dy.sum(0)
+
+
+# ---------------------------------------------------------------- gated feed-forward projections
+#     [g u] = a w,  h = act(g) * u;   dg = dh * u * act'(g),  du = dh * act(g),  da = [dg du] w^T,  dw = a^T [dg du]
+def activation_ref(g, kind):
+    """act(g), act'(g)."""
+    g = np.asarray(g, np.float64)
+    if kind == "silu":
+        s = 0.5 * (1 + np.tanh(0.5 * g))
+        return g * s, s + g * s * (1 - s)
+    from scipy.special import erf
+
+    P = 0.5 * (1 + erf(g / np.sqrt(2)))
+    return g * P, P + g * np.exp(-g * g / 2) / np.sqrt(2 * np.pi)
+
+
+def gated_fwd_ref(a, w, kind):
+    """h, gu."""
+    gu = np.matmul(np.asarray(a, np.float64), np.asarray(w, np.float64))
+    g, u = np.split(gu, 2, 1)
+    return activation_ref(g, kind)[0] * u, gu
+
+
+def gated_bwd_ref(a, w, dh, kind, gu=None):
+    """da, dw, dgu; gu: the projections to start from (None: those of a and w)."""
+    a, w, dh = (np.asarray(t, np.float64) for t in (a, w, dh))
+    g, u = np.split(np.matmul(a, w) if gu is None else np.asarray(gu, np.float64), 2, 1)
+    value, slope = activation_ref(g, kind)
+    dgu = np.concatenate([dh * u * slope, dh * value], 1)
+    return np.matmul(dgu, w.T), np.matmul(a.T, dgu), dgu

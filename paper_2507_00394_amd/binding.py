@@ -19,6 +19,7 @@ EXPORTS = ("helix_attn_fwd", "helix_attn_bwd", "helix_attn_bwd_static", "helix_a
            "helix_attn_bwd_preprocess", "helix_attn_bwd_delta_head", "helix_attn_bwd_dkdv", "helix_attn_bwd_dq",
            "helix_dropout_add_fwd", "helix_dropout_add_bwd", "helix_layer_norm_fwd", "helix_layer_norm_bwd", "helix_layer_norm_bwd_workspace_bytes",
            "helix_dropout_add_layer_norm_fwd", "helix_dropout_add_layer_norm_bwd",
+           "helix_gated_linear_fwd", "helix_gated_linear_bwd", "helix_gated_linear_bwd_workspace_bytes",
            "helix_attn_device_info", "helix_mfma_probe", "helix_mfma_mix_probe", "helix_status_string", "helix_attn_version")
 HELIX_OK = 0
 _lib = None
@@ -71,7 +72,11 @@ def lib() -> ctypes.CDLL:
         L.helix_layer_norm_bwd_workspace_bytes.restype = sz
         L.helix_dropout_add_layer_norm_fwd.argtypes = [vp, ll, vp, ll, vp, ll, fp, fp, vp, ll, fp, fp, i, i, i, f, vp, ll, f, vp]
         L.helix_dropout_add_layer_norm_bwd.argtypes = [vp, ll, vp, ll, vp, ll, fp, fp, fp, vp, ll, vp, ll, fp, fp, vp, sz, i, i, i, f, vp, ll, vp]
-        for name in ("helix_dropout_add_fwd", "helix_dropout_add_bwd", "helix_layer_norm_fwd", "helix_layer_norm_bwd",
+        L.helix_gated_linear_fwd.argtypes = [vp, ll, vp, ll, vp, ll, vp, ll, i, i, i, i, vp]
+        L.helix_gated_linear_bwd.argtypes = [vp, ll, vp, ll, vp, ll, vp, ll, vp, ll, vp, ll, vp, sz, i, i, i, i, vp]
+        L.helix_gated_linear_bwd_workspace_bytes.argtypes = [i, i, i]
+        L.helix_gated_linear_bwd_workspace_bytes.restype = sz
+        for name in ("helix_gated_linear_fwd", "helix_gated_linear_bwd", "helix_dropout_add_fwd", "helix_dropout_add_bwd", "helix_layer_norm_fwd", "helix_layer_norm_bwd",
                      "helix_dropout_add_layer_norm_fwd", "helix_dropout_add_layer_norm_bwd"):
             getattr(L, name).restype = i
         L.helix_attn_bwd_workspace_bytes.argtypes = [i, i, i, i]
@@ -442,3 +447,47 @@ def helix_dropout_add_layer_norm_bwd(dy, ds, s, gamma, mean, rstd, dx, dresidual
     _here(stream, dy, ds, s, gamma, mean, rstd, dx, dresidual, dgamma, dbeta, workspace, rng)
     _raise(lib().helix_dropout_add_layer_norm_bwd(pdy, lddy, pds, ldds, ps, lds, pg, pm, pr, pdx, lddx, pdr, lddr, pdg, pdb, pw, nw, M, E, kind, float(p),
                                                   pn, int(first_row), _stream(stream)), "helix_dropout_add_layer_norm_bwd")
+
+
+# ---------------------------------------------------------------- gated feed-forward projections
+_ACTIVATIONS = {"silu": 0, "gelu": 1}
+
+
+def _gated(a, w, activation):
+    """(M, K, F, activation) of the gated projections."""
+    if activation not in _ACTIVATIONS:
+        raise ValueError(f"activation: need one of {tuple(_ACTIVATIONS)}")
+    if a.dim() != 2 or w.dim() != 2 or w.shape[1] % 2:
+        raise ValueError("need matrices a [M, K] and w [K, 2F]")
+    return a.shape[0], a.shape[1], w.shape[1] // 2, _ACTIVATIONS[activation]
+
+
+def _tall(name, t, rows, cols):
+    """_matrix, where the pitch of a single row counts for nothing."""
+    ptr, ld = _matrix(name, t, rows, cols)
+    return ptr, ld if rows > 1 else cols
+
+
+def helix_gated_linear_fwd(a, w, h, gu=None, activation="silu", stream=None):
+    """h[M,F] <- act(a @ w[:, :F]) * (a @ w[:, F:]); gu[M,2F], if given, <- a @ w for the backward.  bf16, 2-D views with contiguous rows."""
+    M, K, F, act = _gated(a, w, activation)
+    (pa, lda), (pw, ldw), (ph, ldh) = _tall("a", a, M, K), _matrix("w", w, K, 2 * F), _tall("h", h, M, F)
+    pg, ldg = (None, 0) if gu is None else _tall("gu", gu, M, 2 * F)
+    _here(stream, a, w, h, gu)
+    _raise(lib().helix_gated_linear_fwd(pa, lda, pw, ldw, pg, ldg, ph, ldh, M, K, F, act, _stream(stream)), "helix_gated_linear_fwd")
+
+
+def helix_gated_linear_bwd_workspace_bytes(M, K, F) -> int:
+    return int(lib().helix_gated_linear_bwd_workspace_bytes(M, K, F))
+
+
+def helix_gated_linear_bwd(a, w, dh, da, dw, workspace, gu=None, activation="silu", stream=None):
+    """da[M,K], dw[K,2F] <- gradients of helix_gated_linear_fwd for dh[M,F], from the gu it wrote or, without, from a and w alone; workspace:
+    uint8 CUDA tensor of helix_gated_linear_bwd_workspace_bytes(M, K, F) bytes."""
+    M, K, F, act = _gated(a, w, activation)
+    (pa, lda), (pw, ldw), (ph, ldh) = _tall("a", a, M, K), _matrix("w", w, K, 2 * F), _tall("dh", dh, M, F)
+    (pda, ldda), (pdw, lddw) = _tall("da", da, M, K), _matrix("dw", dw, K, 2 * F)
+    pg, ldg = (None, 0) if gu is None else _tall("gu", gu, M, 2 * F)
+    pws, nws = _workspace(workspace)
+    _here(stream, a, w, dh, da, dw, gu, workspace)
+    _raise(lib().helix_gated_linear_bwd(pa, lda, pw, ldw, pg, ldg, ph, ldh, pda, ldda, pdw, lddw, pws, nws, M, K, F, act, _stream(stream)), "helix_gated_linear_bwd")

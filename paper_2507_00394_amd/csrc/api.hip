@@ -135,6 +135,12 @@ int to_dropout(float p, const unsigned long long* rng, long long first_row, int 
   out->first_row = (unsigned)first_row;
   return HELIX_OK;
 }
+// Gated projections: the linear layer's rules with 2F columns, of which F % 64 == 0, and any M.
+int check_gated(int M, int K, int F, int activation, std::initializer_list<std::pair<long long, int>> lds) {
+  if (activation != HELIX_SILU && activation != HELIX_GELU) return HELIX_ERR_BAD_TYPE;
+  if (F < 1 || F > (1 << 19) || M > 0x7fffffff - 256) return HELIX_ERR_BAD_SHAPE;
+  return check_linear(M, K, 2 * F, false, lds);
+}
 int check_eps(float eps) { return std::isfinite(eps) && eps > 0.f ? HELIX_OK : HELIX_ERR_BAD_EPSILON; }
 int check_f32_or_null(const void* p) { return aligned(p, 4) ? HELIX_OK : HELIX_ERR_MISALIGNED; }
 int check_workspace(const void* p, size_t bytes, size_t need) {
@@ -388,6 +394,33 @@ int helix_dropout_add_layer_norm_bwd(const void* dy, long long lddy, const void*
                       lddy, ldds, lds, lddx, lddr, M, E, {}};
   HELIX_TRY(to_dropout(p, rng, first_row, M, &a.drop));
   return launched(helix::launch_norm_bwd(a, (helix::ElementType)type, (hipStream_t)stream));
+}
+
+int helix_gated_linear_fwd(const void* a, long long lda, const void* w, long long ldw, void* gu, long long ldgu,
+                           void* h, long long ldh, int M, int K, int F, int activation, void* stream) {
+  HELIX_TRY(check_bf16_ptrs(a, w, (const void*)h));
+  if (!aligned(gu, 16)) return HELIX_ERR_MISALIGNED;
+  if (F < 1 || F > (1 << 19)) return HELIX_ERR_BAD_SHAPE;   // before 2F is formed
+  HELIX_TRY(check_gated(M, K, F, activation, {{lda, K}, {ldw, 2 * F}, {gu ? ldgu : 2 * F, 2 * F}, {ldh, F}}));
+  const helix::Gated p = {a, w, nullptr, h, gu, lda, ldw, 0, ldh, ldgu, M, K, F};
+  return launched(helix::launch_gated_fwd(p, (helix::Activation)activation, (hipStream_t)stream));
+}
+
+size_t helix_gated_linear_bwd_workspace_bytes(int M, int K, int F) {
+  if (check_gated(M, K, F, HELIX_SILU, {}) != HELIX_OK) return 0;
+  return (helix::gated_bwd_workspace_bytes(M, K, F) + 255) & ~(size_t)255;
+}
+
+int helix_gated_linear_bwd(const void* a, long long lda, const void* w, long long ldw, const void* gu, long long ldgu,
+                           const void* dh, long long lddh, void* da, long long ldda, void* dw, long long lddw,
+                           void* workspace, size_t workspace_bytes, int M, int K, int F, int activation, void* stream) {
+  HELIX_TRY(check_bf16_ptrs(a, w, dh, (const void*)da, (const void*)dw));
+  if (!aligned(gu, 16)) return HELIX_ERR_MISALIGNED;
+  if (F < 1 || F > (1 << 19)) return HELIX_ERR_BAD_SHAPE;   // before 2F is formed
+  HELIX_TRY(check_gated(M, K, F, activation, {{lda, K}, {ldw, 2 * F}, {gu ? ldgu : 2 * F, 2 * F}, {lddh, F}, {ldda, K}, {lddw, 2 * F}}));
+  HELIX_TRY(check_workspace(workspace, workspace_bytes, helix_gated_linear_bwd_workspace_bytes(M, K, F)));
+  const helix::Gated p = {a, w, dh, nullptr, nullptr, lda, ldw, lddh, 0, 0, M, K, F};
+  return launched(helix::launch_gated_bwd(p, gu, ldgu, da, ldda, dw, lddw, workspace, (helix::Activation)activation, (hipStream_t)stream));
 }
 
 int helix_mfma_probe(float* sink, int workgroups, int iters, int random_operands, long long* flops, void* stream) {

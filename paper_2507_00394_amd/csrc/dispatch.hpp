@@ -333,6 +333,13 @@ inline TilePair linear_gradient_tiles(int M, int K, int N, int parts) {
   return TilePair{(TileKind)best->input, (TileKind)best->weight};
 }
 
+// The gated projections: tiles of h of 256 x 128, 128 x 64 and 64 x 64 elements.
+inline TileKind gated_tile(int M, int K, int F) {
+  (void)K;
+  const long long wide = (long long)((M + 255) / 256) * ((F + 127) / 128), middle = (long long)((M + 127) / 128) * ((F + 63) / 64);
+  return wide >= 256 ? TileKind::k256 : middle >= 256 ? TileKind::k128 : TileKind::k64;
+}
+
 // ---------------------------------------------------------------- layer norm's rows
 //
 // How many lanes hold a row, and how many chunks of 8 columns a lane at most: as few lanes as have it in registers, with few registers a lane.

@@ -73,6 +73,10 @@ size_t linear_bwd_workspace_bytes(int M, int K, int N);
 hipError_t launch_linear_bwd(const void* a, long long lda, const void* w, long long ldw, const void* dout, long long ldd, void* da,
                              long long ldda, float* dw, long long lddw, void* workspace, int M, int K, int N, hipStream_t stream);
 
+// The same two products for any M and a bf16 weight gradient (gated.hip); dout has rows of zeros up to the next multiple of 32.
+hipError_t launch_linear_bwd_ragged(const void* a, long long lda, const void* w, long long ldw, const void* dout, long long ldd, void* da,
+                                    long long ldda, void* dw, long long lddw, void* workspace, int M, int K, int N, hipStream_t stream);
+
 // Pure MFMA loop (mfma_probe.hip): `workgroups` x 8 waves x `iters` x 16 independent 32x32x16 bf16 MFMAs.
 long long mfma_probe_flops(int workgroups, int iters);
 hipError_t launch_mfma_probe(float* sink, int workgroups, int iters, bool random_operands, hipStream_t stream);
@@ -111,5 +115,19 @@ hipError_t launch_dropout_add(const void* x, long long ldx, const void* r, long 
                               const Dropout& drop, hipStream_t stream);   // r may be null
 hipError_t launch_norm_fwd(const NormFwd& a, ElementType type, hipStream_t stream);
 hipError_t launch_norm_bwd(const NormBwd& a, ElementType type, hipStream_t stream);
+
+// The gated feed-forward projections (gated.hip): [g u] = a[M][K] w[K][2F], h = act(g) * u.
+enum class Activation { silu, gelu };
+struct Gated {
+  const void *a, *w, *dh;
+  void *h, *gu;   // gu [M][2F]: out; null: g and u are not kept
+  long long lda, ldw, lddh, ldh, ldgu;
+  int M, K, F;
+};
+hipError_t launch_gated_fwd(const Gated& p, Activation act, hipStream_t stream);
+size_t gated_bwd_workspace_bytes(int M, int K, int F);
+// gu: what the forward kept, or null: the projections are computed again.  dw is bf16.
+hipError_t launch_gated_bwd(const Gated& p, const void* gu, long long ldgu, void* da, long long ldda, void* dw, long long lddw, void* workspace, Activation act,
+                            hipStream_t stream);
 
 }  // namespace helix

@@ -80,3 +80,28 @@ def test_gradients_by_differences():
             a[k][idx] += h
             b[k][idx] -= h
             assert (loss(*a) - loss(*b)) / (2 * h) == pytest.approx(want[idx], rel=1e-6, abs=1e-7)
+
+
+@pytest.mark.parametrize("kind", ["silu", "gelu"])
+def test_gated_scalar_loops_and_differences(kind):
+    import math
+
+    rng = np.random.Generator(np.random.Philox(14))
+    M, K, F = 3, 5, 4
+    a, w, dh = rng.standard_normal((M, K)), rng.standard_normal((K, 2 * F)), rng.standard_normal((M, F))
+    act = (lambda g: g / (1 + math.exp(-g))) if kind == "silu" else (lambda g: g * 0.5 * math.erfc(-g / math.sqrt(2)))
+    h, gu = R.gated_fwd_ref(a, w, kind)
+    for i in range(M):
+        for j in range(F):
+            g, u = sum(a[i, k] * w[k, j] for k in range(K)), sum(a[i, k] * w[k, F + j] for k in range(K))
+            assert h[i, j] == pytest.approx(act(g) * u, rel=1e-12, abs=1e-13) and gu[i, j] == pytest.approx(g, abs=1e-13)
+    da, dw, _ = R.gated_bwd_ref(a, w, dh, kind)
+    step = 1e-5
+    for x, grad, loss in ((a, da, lambda t: (dh * R.gated_fwd_ref(t, w, kind)[0]).sum()), (w, dw, lambda t: (dh * R.gated_fwd_ref(a, t, kind)[0]).sum())):
+        for idx in np.ndindex(x.shape):
+            up, down = x.copy(), x.copy()
+            up[idx] += step
+            down[idx] -= step
+            assert (loss(up) - loss(down)) / (2 * step) == pytest.approx(grad[idx], rel=1e-6, abs=1e-8)
+    kept = R.gated_bwd_ref(a, w, dh, kind, gu=gu)
+    assert np.allclose(kept[0], da, rtol=1e-13) and np.allclose(kept[1], dw, rtol=1e-13)
