@@ -53,6 +53,11 @@ def parse():
     ap.add_argument("--qkv-linear", action="store_true",
                     help="time the QKV linear layer of the attention stage (Section 4.2) instead of attention: "
                          "M = --seq tokens, K = --hidden, N = 3 * --share-heads * 128 columns (default 4 heads)")
+    ap.add_argument("--layer-parts", action="store_true",
+                    help="instead of attention, measure what a layer does before and after its attention stage, forward and backward, as "
+                         "one GPU of a sequence-parallel group of --parallel does it on --seq tokens: layer norm; output projection, dropout + "
+                         "residual sum + layer norm, gated projections, down projection, dropout + residual sum")
+    ap.add_argument("--parallel", type=int, default=8, help="--layer-parts: GPUs that share a layer")
     ap.add_argument("--hidden", type=int, default=4096)
     ap.add_argument("--calibration-copy-mib", type=int, default=0,
                     help="before anything is timed, copy this many MiB device to device once: a plain copy of known "
@@ -291,6 +296,82 @@ def linear_bench(args):
     print(json.dumps(out))
 
 
+def layer_parts_bench(args):
+    """Pre- and post-attention of one layer, one GPU's share: the linear layers' columns (output projection: rows) and the feed-forward width are
+    divided among the GPUs, all tokens on each; the row-wise operators run on each GPU's tokens.  F is 8/3 of the hidden size, the width
+    at which three gated matrices hold what two of 4h x h do."""
+    import torch
+
+    from paper_2507_00394_amd import binding as hx
+
+    M, E, tp, p, eps = args.seq, args.hidden, args.parallel, 0.1, 1e-5
+    if M % (32 * tp) or E % (128 * tp):
+        print("--layer-parts needs --seq to be a multiple of 32 x --parallel and --hidden of 128 x --parallel", file=sys.stderr)
+        sys.exit(2)
+    T, Es, F = M // tp, E // tp, -(-8 * E // (3 * tp * 128)) * 128
+    gen = torch.Generator(device="cuda").manual_seed(250700394)
+    rnd = lambda r, c, std=1.0: (torch.randn(r, c, generator=gen, device="cuda", dtype=torch.float32) * std).to(torch.bfloat16)
+    bf = lambda *s: torch.empty(s, dtype=torch.bfloat16, device="cuda")
+    f32 = lambda *s: torch.empty(s, dtype=torch.float32, device="cuda")
+    x, o, dy = rnd(T, E), rnd(M, Es), rnd(T, E)
+    w_o, w_gu, w_down = rnd(Es, E, 0.02), rnd(E, 2 * F, 0.02), rnd(F, E, 0.02)
+    gamma, beta = torch.ones(E, device="cuda"), torch.zeros(E, device="cuda")
+    rng = torch.tensor([250700394, 0], dtype=torch.int64, device="cuda")
+    n1, s1, n2, out, d_s, d_n = (bf(T, E) for _ in range(6))
+    m1, r1, m2, r2 = (f32(T) for _ in range(4))
+    proj, gathered, down, d_proj = bf(M, E), rnd(M, E), bf(M, E), bf(M, E)   # collectives between the calls are not part of this measurement
+    h, d_h, d_o = bf(M, F), bf(M, F), bf(M, Es)
+    dw_o, dw_gu, dw_down, dgamma, dbeta = f32(Es, E), bf(E, 2 * F), f32(F, E), f32(E), f32(E)
+    ws = torch.empty(max(hx.helix_qkv_linear_bwd_workspace_bytes(M, Es, E), hx.helix_qkv_linear_bwd_workspace_bytes(M, F, E),
+                         hx.helix_gated_linear_bwd_workspace_bytes(M, E, F), hx.helix_layer_norm_bwd_workspace_bytes(T, E)), dtype=torch.uint8, device="cuda")
+
+    def pre_forward():
+        hx.helix_layer_norm_fwd(x, gamma, beta, n1, m1, r1, eps)
+
+    def post_forward():
+        hx.helix_qkv_linear_fwd(o, w_o, proj)
+        hx.helix_dropout_add_layer_norm_fwd(proj[:T], x, s1, gamma, beta, n2, m2, r2, p, rng, eps)
+        hx.helix_gated_linear_fwd(gathered, w_gu, h)
+        hx.helix_qkv_linear_fwd(h, w_down, down)
+        hx.helix_dropout_add_fwd(down[:T], s1, out, p, rng)
+
+    def post_backward():   # the gated projections are computed again
+        hx.helix_dropout_add_bwd(dy, d_proj[:T], p, rng)
+        hx.helix_qkv_linear_bwd(h, w_down, gathered, d_h, dw_down, ws)
+        hx.helix_gated_linear_bwd(gathered, w_gu, d_h, d_proj, dw_gu, ws)
+        hx.helix_dropout_add_layer_norm_bwd(d_proj[:T], dy, s1, gamma, m2, r2, proj[:T], d_s, dgamma, dbeta, ws, p, rng)
+        hx.helix_qkv_linear_bwd(o, w_o, gathered, d_o, dw_o, ws)
+
+    def pre_backward():
+        hx.helix_dropout_add_layer_norm_bwd(n1, d_s, x, gamma, m1, r1, d_n, out, dgamma, dbeta, ws, 0.0, None)
+
+    parts = (pre_forward, post_forward, post_backward, pre_backward)
+    for _ in range(args.warmup):
+        for part in parts:
+            part()
+    torch.cuda.synchronize()
+    evs = [[torch.cuda.Event(enable_timing=True) for _ in range(5)] for _ in range(args.steps)]
+    t0 = time.perf_counter()
+    for ev in evs:
+        ev[0].record()
+        for part, e in zip(parts, ev[1:]):
+            part()
+            e.record()
+    torch.cuda.synchronize()
+    wall = time.perf_counter() - t0
+    ms = {part.__name__: float(np.mean([ev[i].elapsed_time(ev[i + 1]) for ev in evs])) for i, part in enumerate(parts)}
+    products = 2 * M * E * (Es + 3 * F)                      # forward; twice that backward, and the gated projections again
+    flops = 3 * products + 4 * M * E * F
+    n_cu, clock_khz = hx.helix_attn_device_info()
+    value = flops / (wall / args.steps) / 1e12
+    print(json.dumps({"metric": "pre- and post-attention of a layer fwd+bwd TFLOP/s, one GPU's share", "value": value, "unit": "TFLOP/s", "n_gpus": 1,
+                      "steps": args.steps, "warmup": args.warmup, "ms_per_step": wall * 1e3 / args.steps, "higher_is_better": True, "scaling": "weak",
+                      "vs_baseline": None, "dtype": "bf16", "data": "synthetic",
+                      "config": {"seq_len": M, "hidden": E, "feed_forward_share": F, "tokens_of_row_wise_operators": T, "parallel": tp, "dropout": p},
+                      "pct_of_bf16_mfma_peak": 100 * value / (n_cu * PEAK_FLOP_PER_CLK_PER_CU * clock_khz / 1e9), "ms": ms,
+                      "t_pre_ms": ms["pre_forward"], "t_post_ms": ms["post_forward"]}))
+
+
 def main():
     args = parse()
     if args.gpus != 1:
@@ -309,6 +390,8 @@ def main():
         torch.empty_like(src).copy_(src)
         torch.cuda.synchronize()
         del src
+    if args.layer_parts:
+        return layer_parts_bench(args)
     if args.qkv_linear:
         return linear_bench(args)
     if args.share_heads:

@@ -303,7 +303,7 @@ int helix_dropout_add_layer_norm_bwd(const void* dy, long long lddy, const void*
  *   dw : bf16 [K][2F] (overwritten, not accumulated), summed in fp32 and rounded once
  * activation: a helix_activation (HELIX_ERR_BAD_TYPE).  Any M >= 1; K a multiple of 128 and F of 64 (HELIX_ERR_BAD_SHAPE).  Pointers and
  * ld* as for helix_qkv_linear_fwd: 16-byte aligned, ld* at least the row length, a multiple of 8, at most 2^22 (HELIX_ERR_BAD_STRIDE).
- * The down projection h -> [M][K] is helix_qkv_linear_fwd / _bwd with F in the place of K.
+ * The down projection h -> [M][K] is helix_qkv_linear_fwd / _bwd with F, then a multiple of 128, in the place of K.
  * workspace: device memory of at least helix_gated_linear_bwd_workspace_bytes(M, K, F) bytes, 256-byte aligned, contents undefined
  * afterwards: [dg du], and what helix_qkv_linear_bwd keeps there.  No atomics: every bit is reproduced. */
 int helix_gated_linear_fwd(const void* a, long long lda, const void* w, long long ldw, void* gu, long long ldgu,

@@ -118,17 +118,21 @@ def main(argv=None):
                     help="measured attention FORWARD time of one micro batch and layer on one GPU (its share of the heads)")
     ap.add_argument("--gemm-tflops", type=float, default=1000.0,
                     help="assumed sustained rate of the dense layers per GPU, to turn Table 1 FLOPs into t_pre, t_post")
+    ap.add_argument("--t-pre-ms", type=float, default=0.0,
+                    help="measured FORWARD time of the layer norm in front of the QKV linear layer on one GPU (`bench.py --layer-parts`: t_pre_ms)")
+    ap.add_argument("--t-post-ms", type=float, default=None,
+                    help="measured FORWARD time of post-attention on one GPU (`bench.py --layer-parts`: t_post_ms), in the place of Table 1's FLOPs at --gemm-tflops")
     ap.add_argument("--sp", type=int, default=8, help="sequence-parallel size inside a stage")
     a = ap.parse_args(argv)
     f = layer_flops(1, a.seq, a.hidden)["forward"]
     rate = a.sp * a.gemm_tflops * 1e9                      # FLOPs per ms of one stage
     t_qkv = f["qkv_linear"] / rate
-    t_post = (f["o_linear"] + f["linear1"] + f["linear2"]) / rate
-    # LayerNorm has no matrix FLOPs.  Layer-wise schedules keep the QKV linear layer (which has a
+    t_post = (f["o_linear"] + f["linear1"] + f["linear2"]) / rate if a.t_post_ms is None else a.t_post_ms
+    # LayerNorm has no matrix FLOPs: it counts where it was measured.  Layer-wise schedules keep the QKV linear layer (which has a
     # backward W) in the pre-attention part; HelixPipe runs it on the attention stage (Section 4.2),
     # so there it counts as attention time and leaves the bubble.
-    parts = {"layerwise": (t_qkv, a.t_attn_ms, t_post), "helix": (0.0, a.t_attn_ms + t_qkv, t_post)}
-    out = {"t_qkv_linear_ms": t_qkv, "t_attention_ms": a.t_attn_ms, "t_post_ms": t_post, "schedules": {}}
+    parts = {"layerwise": (a.t_pre_ms + t_qkv, a.t_attn_ms, t_post), "helix": (a.t_pre_ms, a.t_attn_ms + t_qkv, t_post)}
+    out = {"t_pre_ms": a.t_pre_ms, "t_qkv_linear_ms": t_qkv, "t_attention_ms": a.t_attn_ms, "t_post_ms": t_post, "schedules": {}}
     for sch in SCHEDULES:
         t_pre, t_attn, t_post_ = parts["helix" if sch.startswith("helix") else "layerwise"]
         pr = predict(sch, a.p, a.layers, a.micro_batches, t_pre, t_attn, t_post_)
