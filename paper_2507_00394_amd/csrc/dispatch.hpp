@@ -350,13 +350,32 @@ inline NormRows norm_rows(int cols) {
        : cols <= 8192 ? NormRows::k512x2 : NormRows::k1024x2;
 }
 inline int norm_lanes(NormRows r) { return r == NormRows::k16x2 ? 16 : r == NormRows::k64x2 ? 64 : r == NormRows::k512x2 ? 512 : r == NormRows::k1024x2 ? 1024 : 256; }
-// Workgroups of `threads` that the chip holds at once: 32 waves a compute unit.
-inline int norm_groups_at_once(int threads) { return 256 * 2048 / threads; }
-// Workgroups of the gradient.  Each leaves a slab of partial sums of dgamma and dbeta.
+// Waves of the forward kernel on a SIMD; its registers are limited to what so many leave.  SUM: with dropout and residual sum.  Beyond what keeps the memory
+// busy more of them change little (us with 7 / 5 / 4, SUM 5 / 4 / 3 / 2: layer norm of 131072 x 4096 400 / 386 / 400, 8192 x 5001 34 / 41 / 41, SUM 32768 x 4096 201 /
+// 192 / 190 / 225, 20000 x 900 27.3 / 27.3 / 28.4 / 31.9).
+constexpr int norm_fwd_waves(int L, int NC, bool sum) { return L == 1024 ? 4 : sum ? (NC == 2 ? 4 : 7) : NC == 2 ? 7 : 8; }
+// Workgroups of `threads` that the chip holds at once with so many waves on a SIMD.  More would run when the others have ended, with the chip nearly empty.
+constexpr int groups_at_once(int threads, int waves) { return 256 * (waves * 256 / threads); }
+
+// The gradient: one workgroup to a compute unit, of as many threads as there can be, so of several rows at a time; with few rows
+// of fewer, so that all compute units have some.
+enum class NormBwdRows { k16x2, k64x2, k128x2, k256x2, k512x2, k1024x2 };
+inline NormBwdRows norm_bwd_rows(int cols) {
+  return cols <= 256 ? NormBwdRows::k16x2 : cols <= 1024 ? NormBwdRows::k64x2 : cols <= 2048 ? NormBwdRows::k128x2 : cols <= 4096 ? NormBwdRows::k256x2
+       : cols <= 8192 ? NormBwdRows::k512x2 : NormBwdRows::k1024x2;
+}
+constexpr int kNormBwdThreads = 1024;   // 128 registers each
+inline int norm_bwd_together(int rows, int cols) {
+  const NormBwdRows r = norm_bwd_rows(cols);
+  const int lanes = r == NormBwdRows::k16x2 ? 16 : r == NormBwdRows::k128x2 ? 128 : r == NormBwdRows::k256x2 ? 256 : r == NormBwdRows::k512x2 ? 512 : r == NormBwdRows::k1024x2 ? 1024 : 64;
+  const int most = kNormBwdThreads / lanes, least = lanes < 64 ? 64 / lanes : 1;   // whole waves
+  const int wanted = (int)(((long long)rows + 255) / 256);
+  return wanted >= most ? most : wanted <= least ? least : (wanted + least - 1) / least * least;
+}
+// Its workgroups.  Each leaves a slab of partial sums of dgamma and dbeta.
 inline int norm_bwd_groups(int rows, int cols) {
-  const int lanes = norm_lanes(norm_rows(cols)), threads = lanes > 256 ? lanes : 256, together = threads / lanes;
-  const long long turns = ((long long)rows + together - 1) / together;   // of a workgroup, if there were only one
-  return (int)std::min<long long>(turns, 256 * 1024 / threads);
+  const long long turns = ((long long)rows + norm_bwd_together(rows, cols) - 1) / norm_bwd_together(rows, cols);
+  return (int)std::min<long long>(turns, 256);
 }
 
 }  // namespace helix

@@ -27,13 +27,13 @@ struct Chunk {
   typedef T Vec __attribute__((ext_vector_type(8), aligned(sizeof(T))));
   Vec v;
 };
-// `n` of the 8 elements exist; the others are read as zero and not written.
+// `n` of the 8 elements exist; the others are read as zero and not written.  Loads that do not ask to be kept: 129 us instead of 157 for dropout and sum of 32768 x 4096.
 template <typename T>
 __device__ __forceinline__ Chunk<T> load_chunk(const T* p, int n) {
   Chunk<T> c;
   c.v = (T)0.f;
   if (n >= 8) {
-    c.v = *reinterpret_cast<const typename Chunk<T>::Vec*>(p);
+    c.v = __builtin_nontemporal_load(reinterpret_cast<const typename Chunk<T>::Vec*>(p));
   } else if (n > 0) {
 #pragma unroll
     for (int e = 0; e < 7; e++)
@@ -147,13 +147,13 @@ __device__ __forceinline__ float wave_sum(float x) {
   return x;
 }
 template <int L, int N>
-__device__ __forceinline__ void row_sums(float (&x)[N], float (*red)[N]) {
+__device__ __forceinline__ void row_sums(float (&x)[N], float (*red)[N]) {   // red: this row's
 #pragma unroll
   for (int k = 0; k < N; k++) x[k] = wave_sum<L>(x[k]);
   if constexpr (L > 64) {
     if ((threadIdx.x & 63) == 0)
 #pragma unroll
-      for (int k = 0; k < N; k++) red[threadIdx.x >> 6][k] = x[k];
+      for (int k = 0; k < N; k++) red[threadIdx.x % L >> 6][k] = x[k];
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < N; k++) x[k] = red[0][k];
@@ -164,45 +164,98 @@ __device__ __forceinline__ void row_sums(float (&x)[N], float (*red)[N]) {
   }
 }
 
-constexpr int row_threads(int L) { return L > 256 ? L : 256; }
-// L lanes hold a row, NC chunks each: lane l the chunks l, l + L, ...
+// L lanes hold a row of the matrix, NC chunks each: lane l the chunks l, l + L, ... as far as they are whole.  The columns behind the last whole chunk, seven at
+// most, are one each with the first lanes ("tail"): what a lane does for a chunk has no case for a part of one, which would be most of the code.
 template <int L, int NC>
-struct Rows {
-  static constexpr int THREADS = row_threads(L), PER_GROUP = THREADS / L, WAVES = THREADS / 64, COLS = 8 * L * NC;
+struct Columns {
+  int l, tail, tail_at;   // tail_at: column of this lane's element behind the chunks
+  bool has[NC], has_tail;
+  uint32_t first;         // column of its first chunk
+  __device__ __forceinline__ explicit Columns(int cols) : l(threadIdx.x % L), tail(cols & 7), tail_at((cols & ~7) + l), has_tail(l < tail), first(8 * l) {
+#pragma unroll
+    for (int i = 0; i < NC; i++) has[i] = 8 * (l + L * i) + 8 <= cols;
+  }
+  template <typename T>
+  __device__ __forceinline__ Chunk<T> load(const T* row, int i) const {
+    Chunk<T> c;
+    c.v = (T)0.f;
+    if (has[i]) c.v = *reinterpret_cast<const typename Chunk<T>::Vec*>(row + (first + 8 * L * i));
+    return c;
+  }
+  // ONCE: results of one use, which need not push anything out of the caches (gradient of dropout, sum and norm, 131072 x 4096: 1037 -> 965 us; the
+  // 32 bytes that a lane has of a 4-byte type go out in two halves, which the L2 had better join)
+  template <bool ONCE = false, typename T>
+  __device__ __forceinline__ void store(T* row, int i, const f32x8& x) const {
+    auto* const p = reinterpret_cast<typename Chunk<T>::Vec*>(row + (first + 8 * L * i));
+    const auto v = __builtin_convertvector(x, typename Chunk<T>::Vec);
+    if (has[i]) {
+      if constexpr (ONCE && sizeof(T) == 2) __builtin_nontemporal_store(v, p);
+      else *p = v;
+    }
+  }
+  template <typename T>
+  __device__ __forceinline__ float load_tail(const T* row) const { return has_tail ? (float)row[tail_at] : 0.f; }
+  template <typename T>
+  __device__ __forceinline__ void store_tail(T* row, float x) const {
+    if (has_tail) row[tail_at] = (T)x;
+  }
+  __device__ __forceinline__ uint32_t chunk(int i) const { return l + L * i; }
+  // keep * x * scale for this lane's element of the tail
+  __device__ __forceinline__ float apply_tail(const Generator& gen, float x, uint32_t row) const {
+    if (!gen.cut) return x;
+    const u32x4 bits = gen.block(tail_at >> 3, row);
+    const uint32_t w = tail_at & 4 ? (tail_at & 2 ? bits[3] : bits[2]) : (tail_at & 2 ? bits[1] : bits[0]);
+    return (tail_at & 1 ? w >> 16 : w & 0xffffu) >= gen.cut ? x * gen.scale : 0.f;
+  }
 };
+// Which of a workgroup's rows this lane works on: in a scalar register where a wave has no other, and with it the rows' addresses.
+template <int L>
+__device__ __forceinline__ int row_of_lane() {
+  if constexpr (L >= 64) return __builtin_amdgcn_readfirstlane(threadIdx.x / L);
+  else return threadIdx.x / L;
+}
+constexpr int row_threads(int L) { return L > 256 ? L : 256; }
 
 template <typename T, int L, int NC, bool SUM>
-__global__ void __launch_bounds__(row_threads(L)) layer_norm_fwd_kernel(NormFwd a) {
-  using R = Rows<L, NC>;
-  __shared__ float red[2][R::WAVES][1];
-  const int l = threadIdx.x % L, sub = threadIdx.x / L;
-  const T *const x = (const T*)a.x, *const r = (const T*)a.r;
-  T *const s = (T*)a.s, *const y = (T*)a.y;
-  int n[NC];
+__global__ void __launch_bounds__(row_threads(L)) __attribute__((amdgpu_waves_per_eu(norm_fwd_waves(L, NC, SUM), norm_fwd_waves(L, NC, SUM)))) layer_norm_fwd_kernel(NormFwd a) {
+  constexpr int TOGETHER = row_threads(L) / L;
+  __shared__ float red[2][row_threads(L) / 64][1];
+  const int sub = row_of_lane<L>();
+  const Columns<L, NC> at(a.cols);
   f32x8 gamma[NC], beta[NC];
 #pragma unroll
   for (int i = 0; i < NC; i++) {
-    n[i] = a.cols - 8 * (l + L * i);
-    gamma[i] = widen(load_chunk(a.gamma + 8 * (l + L * i), n[i]));
-    beta[i] = widen(load_chunk(a.beta + 8 * (l + L * i), n[i]));
+    gamma[i] = widen(at.load(a.gamma, i));
+    beta[i] = widen(at.load(a.beta, i));
   }
+  const float gamma_tail = at.load_tail(a.gamma), beta_tail = at.load_tail(a.beta);
   const Generator gen(a.drop);
   const float over = 1.f / (float)a.cols;
-  for (unsigned row = blockIdx.x * R::PER_GROUP + sub; row < (unsigned)a.rows; row += gridDim.x * R::PER_GROUP) {
+  for (unsigned row = blockIdx.x * TOGETHER + sub; row < (unsigned)a.rows; row += gridDim.x * TOGETHER) {
+    const T *const x = (const T*)a.x + (size_t)row * a.ldx, *const r = (const T*)a.r + (size_t)row * a.ldr;
+    T *const s = (T*)a.s + (size_t)row * a.lds, *const y = (T*)a.y + (size_t)row * a.ldy;
     f32x8 v[NC];
+    float vt = 0.f;
     Chunk<T> xc[NC], rc[NC];
 #pragma unroll
     for (int i = 0; i < NC; i++) {
-      xc[i] = load_chunk(x + (size_t)row * a.ldx + 8 * (l + L * i), n[i]);
-      if (SUM) rc[i] = load_chunk(r + (size_t)row * a.ldr + 8 * (l + L * i), n[i]);
+      xc[i] = at.load(x, i);
+      if (SUM) rc[i] = at.load(r, i);
     }
-    float sum[1] = {0.f}, var[1] = {0.f};
+    if (at.tail) {
+      vt = at.load_tail(x);
+      if (SUM) {
+        vt = at.load_tail(r) + at.apply_tail(gen, vt, row);
+        at.store_tail(s, vt);
+      }
+    }
+    float sum[1] = {vt}, var[1] = {0.f};
 #pragma unroll
     for (int i = 0; i < NC; i++) {
       v[i] = widen(xc[i]);
       if (SUM) {
-        v[i] = widen(rc[i]) + gen.apply(v[i], l + L * i, row);
-        store_chunk(s + (size_t)row * a.lds + 8 * (l + L * i), n[i], v[i]);
+        v[i] = widen(rc[i]) + gen.apply(v[i], at.chunk(i), row);
+        at.template store<true>(s, i, v[i]);
       }
 #pragma unroll
       for (int e = 0; e < 8; e++) sum[0] += v[i][e];   // columns that do not exist are zero
@@ -211,159 +264,207 @@ __global__ void __launch_bounds__(row_threads(L)) layer_norm_fwd_kernel(NormFwd 
     row_sums<L>(sum, red[0]);
     const float mean = sum[0] * over;
 #pragma unroll
-    for (int i = 0; i < NC; i++)
+    for (int i = 0; i < NC; i++) {
+      v[i] -= mean;
+      if (at.has[i])
 #pragma unroll
-      for (int e = 0; e < 8; e++) {
-        v[i][e] -= mean;
-        if (e < n[i]) var[0] = fmaf(v[i][e], v[i][e], var[0]);
-      }
+        for (int e = 0; e < 8; e++) var[0] = fmaf(v[i][e], v[i][e], var[0]);
+    }
+    vt -= mean;
+    if (at.has_tail) var[0] = fmaf(vt, vt, var[0]);
     row_sums<L>(var, red[1]);
     const float rstd = 1.f / sqrtf(fmaf(var[0], over, a.eps));
 #pragma unroll
-    for (int i = 0; i < NC; i++) store_chunk(y + (size_t)row * a.ldy + 8 * (l + L * i), n[i], v[i] * rstd * gamma[i] + beta[i]);
-    if (l == 0 && a.mean) a.mean[row] = mean;
-    if (l == 0 && a.rstd) a.rstd[row] = rstd;
+    for (int i = 0; i < NC; i++) at.template store<true>(y, i, v[i] * rstd * gamma[i] + beta[i]);
+    if (at.tail) at.store_tail(y, vt * rstd * gamma_tail + beta_tail);
+    if (at.l == 0 && a.mean) a.mean[row] = mean;
+    if (at.l == 0 && a.rstd) a.rstd[row] = rstd;
   }
 }
 
 // Gradient.  With xh = (x - mean) * rstd and g = dy * gamma:
 //   dx = rstd * (g - mean(g) - xh * mean(g * xh)),   dgamma = sum over rows of dy * xh,   dbeta = sum over rows of dy.
 // SUM (x is the sum s): what came to s directly, ds, is added, and dx = keep * scale * dr for the branch that was dropped out.
-// A thread keeps its columns' sums over the rows of its workgroup; they go to `partial` [gridDim.x][2][cols], which
-// sum_partials_kernel adds up in a fixed order.
+//
+// A lane keeps its columns' sums over all rows that it works on.  A compute unit has one workgroup, of as many rows at a time as it has waves for, so that
+// few partial sums are left: the workgroup adds up its rows' and leaves one slab, `partial` [gridDim.x][2][cols], and sum_partials_kernel adds the slabs up in a fixed
+// order.  Up to 4096 columns a wave has a row to itself and needs no barrier.  gamma waits in LDS for all of them: its registers are the sums'.
 template <typename T, int L, int NC, bool SUM>
-__global__ void __launch_bounds__(row_threads(L)) layer_norm_bwd_kernel(NormBwd a) {
-  using R = Rows<L, NC>;
-  __shared__ float red[2][R::WAVES][2];
-  const int l = threadIdx.x % L, sub = threadIdx.x / L;
-  const T *const x = (const T*)a.x, *const dy = (const T*)a.dy, *const ds = (const T*)a.ds;
-  T *const dx = (T*)a.dx, *const dr = (T*)a.dr;
-  int n[NC];
+__global__ void __launch_bounds__(kNormBwdThreads) layer_norm_bwd_kernel(NormBwd a) {
+  constexpr int COLS = 8 * L * NC, MOST = kNormBwdThreads / L;   // MOST rows at a time
+  __shared__ __align__(16) float lds[(MOST > 2 ? MOST / 2 : 1) * COLS];
+  __shared__ float red[2][kNormBwdThreads / 64][2], tails[2][MOST][8];
+  const int sub = row_of_lane<L>(), together = blockDim.x / L;
+  const Columns<L, NC> at(a.cols);
   f32x8 dgamma[NC], dbeta[NC];
-  // 1024 threads have 128 registers each, too few for gamma beside the sums: there it waits in LDS, 16 bytes to a lane and access
-  constexpr bool IN_LDS = L == 1024;
-  __shared__ f32x4 gamma_lds[IN_LDS ? 2 * NC : 1][IN_LDS ? L : 1];
-  f32x8 gamma_reg[IN_LDS ? 1 : NC];
+  // a chunk is two halves of 16 bytes, L lanes' first halves one behind the other, then their second ones
+  if (sub == 0)
 #pragma unroll
-  for (int i = 0; i < NC; i++) {
-    n[i] = a.cols - 8 * (l + L * i);
-    const f32x8 g = widen(load_chunk(a.gamma + 8 * (l + L * i), n[i]));
-    if constexpr (IN_LDS) {   // a lane reads what it wrote itself: no barrier
-      gamma_lds[2 * i][l] = __builtin_shufflevector(g, g, 0, 1, 2, 3);
-      gamma_lds[2 * i + 1][l] = __builtin_shufflevector(g, g, 4, 5, 6, 7);
-    } else {
-      gamma_reg[i] = g;
+    for (int i = 0; i < NC; i++) {
+      const f32x8 g = widen(at.load(a.gamma, i));
+      f32x4* const to = reinterpret_cast<f32x4*>(lds) + 2 * i * L + at.l;
+      to[0] = __builtin_shufflevector(g, g, 0, 1, 2, 3);
+      to[L] = __builtin_shufflevector(g, g, 4, 5, 6, 7);
     }
-    dgamma[i] = dbeta[i] = 0.f;
-  }
-  constexpr bool LATE = IN_LDS;   // for the same reason ds is read where it is added
-  auto gamma = [&](int i) __attribute__((always_inline)) {
-    if constexpr (IN_LDS) return __builtin_shufflevector(gamma_lds[2 * i][l], gamma_lds[2 * i + 1][l], 0, 1, 2, 3, 4, 5, 6, 7);
-    else return gamma_reg[i];
+  auto gamma_of = [&](int i, int lane) __attribute__((always_inline)) {
+    const f32x4* const p = reinterpret_cast<const f32x4*>(lds) + 2 * i * L + lane;
+    return __builtin_shufflevector(p[0], p[L], 0, 1, 2, 3, 4, 5, 6, 7);
   };
+#pragma unroll
+  for (int i = 0; i < NC; i++) dgamma[i] = dbeta[i] = 0.f;
+  const float gamma_tail = at.load_tail(a.gamma);
+  float dgamma_tail = 0.f, dbeta_tail = 0.f;
   const Generator gen(a.drop);
   const float over = 1.f / (float)a.cols;
   int turn = 0;
-  for (unsigned row = blockIdx.x * R::PER_GROUP + sub; row < (unsigned)a.rows; row += gridDim.x * R::PER_GROUP) {
-    Chunk<T> xc[NC], gc[NC], sc[NC];
+  __syncthreads();
+  for (unsigned first = blockIdx.x * together; first < (unsigned)a.rows; first += gridDim.x * together) {
+    const unsigned row = first + sub;
+    if (row >= (unsigned)a.rows) {   // in the last turn only
+      if constexpr (L > 64) __syncthreads();   // that of row_sums
+      continue;
+    }
+    const T *const dy = (const T*)a.dy + (size_t)row * a.lddy, *const x = (const T*)a.x + (size_t)row * a.ldx;
+    Chunk<T> xc[NC], gc[NC];
+    float xt = 0.f, gt = 0.f;
     const float mean = a.mean[row], rstd = a.rstd[row];
 #pragma unroll
     for (int i = 0; i < NC; i++) {
-      gc[i] = load_chunk(dy + (size_t)row * a.lddy + 8 * (l + L * i), n[i]);
-      xc[i] = load_chunk(x + (size_t)row * a.ldx + 8 * (l + L * i), n[i]);
-      if (SUM && !LATE && ds) sc[i] = load_chunk(ds + (size_t)row * a.ldds + 8 * (l + L * i), n[i]);
+      gc[i] = at.load(dy, i);
+      xc[i] = at.load(x, i);
     }
     float sums[2] = {0.f, 0.f};   // of g and of g * xh
+    int lane = at.l;
+    pin(lane);   // gamma is read here, not once for all rows into registers
+    if (at.tail) {
+      xt = (at.load_tail(x) - mean) * rstd;
+      gt = at.load_tail(dy);
+      dgamma_tail = fmaf(gt, xt, dgamma_tail);
+      dbeta_tail += gt;
+      gt *= gamma_tail;
+      sums[0] = gt;
+      sums[1] = gt * xt;
+    }
 #pragma unroll
     for (int i = 0; i < NC; i++) {
-      const f32x8 d = widen(gc[i]), xh = (widen(xc[i]) - mean) * rstd, gm = gamma(i);
+      const f32x8 d = widen(gc[i]), xh = (widen(xc[i]) - mean) * rstd, gamma = gamma_of(i, lane);
       dbeta[i] += d;
 #pragma unroll
       for (int e = 0; e < 8; e++) {   // dy and gamma are zero in columns that do not exist
         dgamma[i][e] = fmaf(d[e], xh[e], dgamma[i][e]);
-        const float g = d[e] * gm[e];
+        const float g = d[e] * gamma[e];
         sums[0] += g;
         sums[1] = fmaf(g, xh[e], sums[1]);
       }
+      pin(dgamma[i]);   // added here, not when the row is finished
+      pin(dbeta[i]);
     }
-    row_sums<L>(sums, red[turn]);
+    row_sums<L>(sums, red[turn] + (L > 64 ? sub * (L / 64) : 0));
     turn ^= 1;
+    T* const dx = (T*)a.dx + (size_t)row * a.lddx;
     const float mean_g = sums[0] * over, mean_gx = sums[1] * over;
+    pin(lane);
+#pragma unroll
+    for (int i = 0; i < NC; i++) {   // what is made of them above is made again: it would take twice their registers
+      pin(xc[i].v);
+      pin(gc[i].v);
+    }
 #pragma unroll
     for (int i = 0; i < NC; i++) {
-      f32x8 d = (widen(gc[i]) * gamma(i) - mean_g - (widen(xc[i]) - mean) * rstd * mean_gx) * rstd;
+      f32x8 d = (widen(gc[i]) * gamma_of(i, lane) - mean_g - (widen(xc[i]) - mean) * rstd * mean_gx) * rstd;
       if (SUM) {
-        if (LATE && ds) sc[i] = load_chunk(ds + (size_t)row * a.ldds + 8 * (l + L * i), n[i]);
-        if (ds) d += widen(sc[i]);
-        store_chunk(dr + (size_t)row * a.lddr + 8 * (l + L * i), n[i], d);
-        d = gen.apply(d, l + L * i, row);
+        if (a.ds) d += widen(at.load((const T*)a.ds + (size_t)row * a.ldds, i));
+        at.template store<true>((T*)a.dr + (size_t)row * a.lddr, i, d);
+        d = gen.apply(d, at.chunk(i), row);
       }
-      store_chunk(dx + (size_t)row * a.lddx + 8 * (l + L * i), n[i], d);
+      at.template store<true>(dx, i, d);
+    }
+    if (at.tail) {
+      float d = (gt - mean_g - xt * mean_gx) * rstd;
+      if (SUM) {
+        if (a.ds) d += at.load_tail((const T*)a.ds + (size_t)row * a.ldds);
+        at.store_tail((T*)a.dr + (size_t)row * a.lddr, d);
+        d = at.apply_tail(gen, d, row);
+      }
+      at.store_tail(dx, d);
     }
   }
   float* const out = a.partial + (size_t)blockIdx.x * 2 * a.cols;
-  if constexpr (R::PER_GROUP == 1) {
+  if (at.has_tail) {
+    tails[0][sub][at.l] = dgamma_tail;
+    tails[1][sub][at.l] = dbeta_tail;
+  }
 #pragma unroll
-    for (int i = 0; i < NC; i++) {
-      store_chunk(out + 8 * (l + L * i), n[i], dgamma[i]);
-      store_chunk(out + a.cols + 8 * (l + L * i), n[i], dbeta[i]);
-    }
-  } else {
-    __shared__ float all[R::PER_GROUP][R::COLS];
-#pragma unroll
-    for (int which = 0; which < 2; which++) {
-      if (which) __syncthreads();
-#pragma unroll
-      for (int i = 0; i < NC; i++)
-#pragma unroll
-        for (int e = 0; e < 8; e++) all[sub][8 * (l + L * i) + e] = which ? dbeta[i][e] : dgamma[i][e];
+  for (int which = 0; which < 2; which++) {
+    f32x8(&sum)[NC] = which ? dbeta : dgamma;
+    for (int left = together; left > 1; left = (left + 1) / 2) {   // the upper half of the rows' sums is added to the lower
+      const int half = (left + 1) / 2;
       __syncthreads();
-      for (int c = threadIdx.x; c < a.cols; c += R::THREADS) {
-        float t = all[0][c];
+      f32x4* const mine = reinterpret_cast<f32x4*>(lds) + (size_t)(sub >= half ? sub - half : sub) * (COLS / 4) + at.l;
+      if (sub >= half && sub < left)
 #pragma unroll
-        for (int g = 1; g < R::PER_GROUP; g++) t += all[g][c];
-        out[which * a.cols + c] = t;
+        for (int i = 0; i < NC; i++) {
+          mine[2 * i * L] = __builtin_shufflevector(sum[i], sum[i], 0, 1, 2, 3);
+          mine[(2 * i + 1) * L] = __builtin_shufflevector(sum[i], sum[i], 4, 5, 6, 7);
+        }
+      __syncthreads();
+      if (sub + half < left)
+#pragma unroll
+        for (int i = 0; i < NC; i++) sum[i] += __builtin_shufflevector(mine[2 * i * L], mine[(2 * i + 1) * L], 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+    if (sub == 0) {
+#pragma unroll
+      for (int i = 0; i < NC; i++) at.store(out + which * a.cols, i, sum[i]);
+      if (at.has_tail) {   // written above, in front of a barrier unless this is the only row
+        float t = tails[which][0][at.l];
+        for (int g = 1; g < together; g++) t += tails[which][g][at.l];
+        at.store_tail(out + which * a.cols, t);
       }
     }
   }
 }
 
-// dgamma and dbeta: the sums of `groups` slabs of 2 * cols floats.  32 columns to a workgroup, eight threads to a column.
-__global__ void __launch_bounds__(256) sum_partials_kernel(const float* __restrict__ partial, int groups, int cols, float* __restrict__ dgamma, float* __restrict__ dbeta) {
-  __shared__ float all[8][32];
+// dgamma and dbeta: the sums of `groups` slabs of 2 * cols floats.  32 columns to a workgroup, 32 threads to a column, eight loads of each in flight: it is
+// latency that counts here (eight threads to a column and a load at a time: 33 us for 1024 slabs of 2 x 2048 columns).
+constexpr int kSumParts = 32;
+__global__ void __launch_bounds__(32 * kSumParts) sum_partials_kernel(const float* __restrict__ partial, int groups, int cols, float* __restrict__ dgamma, float* __restrict__ dbeta) {
+  __shared__ float all[kSumParts][32];
   const int lane = threadIdx.x & 31, part = threadIdx.x >> 5;
   const int c = blockIdx.x * 32 + lane;
-  float t = 0.f;
+  float t[8] = {};
   if (c < 2 * cols)
-    for (int g = part; g < groups; g += 8) t += partial[(size_t)g * 2 * cols + c];
-  all[part][lane] = t;
+    for (int g = part; g < groups; g += 8 * kSumParts)
+#pragma unroll
+      for (int u = 0; u < 8; u++)
+        if (g + u * kSumParts < groups) t[u] += partial[(size_t)(g + u * kSumParts) * 2 * cols + c];
+  all[part][lane] = ((t[0] + t[1]) + (t[2] + t[3])) + ((t[4] + t[5]) + (t[6] + t[7]));
   __syncthreads();
   if (part == 0 && c < 2 * cols) {
+    float sum = all[0][lane];
 #pragma unroll
-    for (int p = 1; p < 8; p++) t += all[p][lane];
-    if (c < cols) dgamma[c] = t;
-    else dbeta[c - cols] = t;
+    for (int p = 1; p < kSumParts; p++) sum += all[p][lane];
+    if (c < cols) dgamma[c] = sum;
+    else dbeta[c - cols] = sum;
   }
 }
 
 template <typename T, int L, int NC>
 hipError_t launch_fwd_rows(const NormFwd& a, hipStream_t stream) {
-  using R = Rows<L, NC>;
-  const long long groups = ((long long)a.rows + R::PER_GROUP - 1) / R::PER_GROUP;
-  const unsigned grid = (unsigned)std::min<long long>(groups, norm_groups_at_once(R::THREADS));
-  if (a.s) hipLaunchKernelGGL((layer_norm_fwd_kernel<T, L, NC, true>), dim3(grid), dim3(R::THREADS), 0, stream, a);
-  else hipLaunchKernelGGL((layer_norm_fwd_kernel<T, L, NC, false>), dim3(grid), dim3(R::THREADS), 0, stream, a);
+  constexpr int THREADS = row_threads(L), TOGETHER = THREADS / L;
+  const long long groups = ((long long)a.rows + TOGETHER - 1) / TOGETHER;
+  const unsigned grid = (unsigned)std::min<long long>(groups, groups_at_once(THREADS, norm_fwd_waves(L, NC, a.s != nullptr)));
+  if (a.s) hipLaunchKernelGGL((layer_norm_fwd_kernel<T, L, NC, true>), dim3(grid), dim3(THREADS), 0, stream, a);
+  else hipLaunchKernelGGL((layer_norm_fwd_kernel<T, L, NC, false>), dim3(grid), dim3(THREADS), 0, stream, a);
   return hipGetLastError();
 }
 template <typename T, int L, int NC>
 hipError_t launch_bwd_rows(const NormBwd& a, hipStream_t stream) {
-  using R = Rows<L, NC>;
-  const unsigned grid = (unsigned)norm_bwd_groups(a.rows, a.cols);
-  if (a.dr) hipLaunchKernelGGL((layer_norm_bwd_kernel<T, L, NC, true>), dim3(grid), dim3(R::THREADS), 0, stream, a);
-  else hipLaunchKernelGGL((layer_norm_bwd_kernel<T, L, NC, false>), dim3(grid), dim3(R::THREADS), 0, stream, a);
-  hipError_t e = hipGetLastError();
+  const int together = norm_bwd_together(a.rows, a.cols), grid = norm_bwd_groups(a.rows, a.cols);
+  if (a.dr) hipLaunchKernelGGL((layer_norm_bwd_kernel<T, L, NC, true>), dim3((unsigned)grid), dim3((unsigned)(together * L)), 0, stream, a);
+  else hipLaunchKernelGGL((layer_norm_bwd_kernel<T, L, NC, false>), dim3((unsigned)grid), dim3((unsigned)(together * L)), 0, stream, a);
+  const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(sum_partials_kernel, dim3((unsigned)((2 * a.cols + 31) / 32)), dim3(256), 0, stream, a.partial, (int)grid, a.cols, a.dgamma, a.dbeta);
+  hipLaunchKernelGGL(sum_partials_kernel, dim3((unsigned)((2 * a.cols + 31) / 32)), dim3(32 * kSumParts), 0, stream, a.partial, grid, a.cols, a.dgamma, a.dbeta);
   return hipGetLastError();
 }
 
@@ -380,12 +481,12 @@ hipError_t norm_fwd(const NormFwd& a, hipStream_t stream) {
 }
 template <typename T>
 hipError_t norm_bwd(const NormBwd& a, hipStream_t stream) {
-  switch (norm_rows(a.cols)) {
-    case NormRows::k16x2: return launch_bwd_rows<T, 16, 2>(a, stream);
-    case NormRows::k64x2: return launch_bwd_rows<T, 64, 2>(a, stream);
-    case NormRows::k256x1: return launch_bwd_rows<T, 256, 1>(a, stream);
-    case NormRows::k256x2: return launch_bwd_rows<T, 256, 2>(a, stream);
-    case NormRows::k512x2: return launch_bwd_rows<T, 512, 2>(a, stream);
+  switch (norm_bwd_rows(a.cols)) {
+    case NormBwdRows::k16x2: return launch_bwd_rows<T, 16, 2>(a, stream);
+    case NormBwdRows::k64x2: return launch_bwd_rows<T, 64, 2>(a, stream);
+    case NormBwdRows::k128x2: return launch_bwd_rows<T, 128, 2>(a, stream);
+    case NormBwdRows::k256x2: return launch_bwd_rows<T, 256, 2>(a, stream);
+    case NormBwdRows::k512x2: return launch_bwd_rows<T, 512, 2>(a, stream);
     default: return launch_bwd_rows<T, 1024, 2>(a, stream);
   }
 }
