@@ -327,87 +327,99 @@ def helix_qkv_linear_bwd(a, w, dqkv, da, dw, workspace=None, stream=None):
 
 
 # ---------------------------------------------------------------- row-wise operators
+# Tensors have to be on the current device, whose stream the calls go to (a tensor in host memory is on device -1).
 _TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 
 
-def _here(stream, *tensors):
-    """Every tensor (None: left out) lives on the current device, whose stream the call goes to."""
+def _current(t, stream):
+    """The current device; `t` is the call's first tensor."""
+    if not t.is_cuda:
+        raise ValueError("need CUDA tensors")
     device = torch.cuda.current_device() if _device is None else _device()
     if stream is not None and stream.device_index != device:
-        raise ValueError(f"stream: belongs to device {stream.device_index}, the current one is {device}")
-    for t in tensors:
-        if t is not None and t.get_device() != device:
-            raise ValueError(f"a tensor is on {t.device}, the current device is cuda:{device}")
+        raise ValueError(f"stream: belongs to device {stream.device_index}, the current device is {device}")
+    return device
 
 
-def _activation(name, t, like):
-    """(pointer, elements between rows) of a 2-D device matrix with the type and shape of `like` whose rows are contiguous."""
-    if not t.is_cuda or t.dtype is not like.dtype or t.dim() != 2 or t.shape != like.shape:
-        raise ValueError(f"{name}: need a CUDA {like.dtype} matrix of shape {tuple(like.shape)}")
-    rows, cols = t.shape
-    ld, one = t.stride()
-    if one != 1 and cols > 1:
-        raise ValueError(f"{name}: need contiguous rows")
-    return t.data_ptr(), ld if rows > 1 else max(ld, cols)   # a single row has no next one
+def _refuse(name, t, device, what):
+    if not t.is_cuda:
+        raise ValueError(f"{name}: need a CUDA tensor")
+    if t.get_device() != device:
+        raise ValueError(f"{name}: is on {t.device}, the current device is cuda:{device}")
+    raise ValueError(f"{name}: need {what}")
 
 
 def _rows(name, t):
-    """(rows, columns, type) of an activation."""
+    """(shape, element type) of an activation."""
     if t.dim() != 2 or t.dtype not in _TYPES:
         raise ValueError(f"{name}: need a matrix of bfloat16, float16 or float32")
-    return t.shape[0], t.shape[1], _TYPES[t.dtype]
+    return t.shape, t.dtype
 
 
-def _generator(rng):
-    """rng: None, or a CUDA int64 tensor with the two elements seed and offset."""
+def _activation(name, t, shape, dtype, device):
+    """(pointer, elements between rows) of a 2-D device matrix whose rows are contiguous."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device:
+        _refuse(name, t, device, f"a {dtype} matrix of shape {tuple(shape)}")
+    ld, one = t.stride()
+    if one != 1 and shape[1] > 1:
+        raise ValueError(f"{name}: need contiguous rows")
+    return t.data_ptr(), ld if shape[0] > 1 else max(ld, shape[1])   # a single row has no next one
+
+
+def _vector(name, t, n, device):
+    """Pointer of n contiguous fp32 values."""
+    if t.dtype is not _F32 or t.dim() != 1 or t.numel() != n or not t.is_contiguous() or t.get_device() != device:
+        _refuse(name, t, device, f"a contiguous float32 vector of {n} elements")
+    return t.data_ptr()
+
+
+def _generator(rng, device):
+    """rng: None, or an int64 tensor with the two elements seed and offset."""
     if rng is None:
         return None
-    if rng.dtype is not torch.int64 or not rng.is_cuda or not rng.is_contiguous() or rng.numel() != 2:
-        raise ValueError("rng: need a contiguous CUDA int64 tensor of two elements, seed and offset")
+    if rng.dtype is not torch.int64 or rng.numel() != 2 or not rng.is_contiguous() or rng.get_device() != device:
+        _refuse("rng", rng, device, "a contiguous int64 tensor of two elements, seed and offset")
     return rng.data_ptr()
 
 
-def _workspace(workspace):
-    if workspace.dtype is not torch.uint8 or not workspace.is_cuda or not workspace.is_contiguous():
-        raise ValueError("workspace: need a contiguous CUDA uint8 tensor")
+def _workspace(workspace, device):
+    if workspace.dtype is not torch.uint8 or not workspace.is_contiguous() or workspace.get_device() != device:
+        _refuse("workspace", workspace, device, "a contiguous uint8 tensor")
     return workspace.data_ptr(), workspace.numel()
-
-
-def _statistics(M, E, **tensors):
-    """Pointers of fp32 vectors: mean and rstd have M elements, the others E; None stays None."""
-    for name, t in tensors.items():
-        if t is not None:
-            _check_f32(name, t, (M if name in ("mean", "rstd") else E,))
-    return [_ptr(t) for t in tensors.values()]
 
 
 def helix_dropout_add_fwd(x, residual, out, p, rng, first_row=0, stream=None):
     """out[M,E] <- residual + dropout(x); residual None: dropout(x).  rng: CUDA int64 tensor [seed, offset] (None where p == 0);
     row i takes the random numbers of row first_row + i."""
-    M, E, kind = _rows("x", x)
-    (px, ldx), (po, ldo) = _activation("x", x, x), _activation("out", out, x)
-    pr, ldr = (None, 0) if residual is None else _activation("residual", residual, x)
-    pg = _generator(rng)
-    _here(stream, x, residual, out, rng)
-    _raise(lib().helix_dropout_add_fwd(px, ldx, pr, ldr, po, ldo, M, E, kind, float(p), pg, int(first_row), _stream(stream)), "helix_dropout_add_fwd")
+    dev = _current(x, stream)
+    shape, dtype = _rows("x", x)
+    px, ldx = _activation("x", x, shape, dtype, dev)
+    pr, ldr = (None, 0) if residual is None else _activation("residual", residual, shape, dtype, dev)
+    po, ldo = _activation("out", out, shape, dtype, dev)
+    _raise(lib().helix_dropout_add_fwd(px, ldx, pr, ldr, po, ldo, shape[0], shape[1], _TYPES[dtype], float(p), _generator(rng, dev), int(first_row), _stream(stream)),
+           "helix_dropout_add_fwd")
 
 
 def helix_dropout_add_bwd(dout, dx, p, rng, first_row=0, stream=None):
     """dx[M,E] <- gradient of the dropped-out branch; the residual's gradient is dout itself."""
-    M, E, kind = _rows("dout", dout)
-    (pg, ldg), (px, ldx) = _activation("dout", dout, dout), _activation("dx", dx, dout)
-    pr = _generator(rng)
-    _here(stream, dout, dx, rng)
-    _raise(lib().helix_dropout_add_bwd(pg, ldg, px, ldx, M, E, kind, float(p), pr, int(first_row), _stream(stream)), "helix_dropout_add_bwd")
+    dev = _current(dout, stream)
+    shape, dtype = _rows("dout", dout)
+    pg, ldg = _activation("dout", dout, shape, dtype, dev)
+    px, ldx = _activation("dx", dx, shape, dtype, dev)
+    _raise(lib().helix_dropout_add_bwd(pg, ldg, px, ldx, shape[0], shape[1], _TYPES[dtype], float(p), _generator(rng, dev), int(first_row), _stream(stream)),
+           "helix_dropout_add_bwd")
 
 
 def helix_layer_norm_fwd(x, gamma, beta, y, mean, rstd, eps=1e-5, stream=None):
     """y[M,E], mean[M], rstd[M] <- layer norm of the rows of x; gamma, beta: fp32 [E].  mean and rstd may be None."""
-    M, E, kind = _rows("x", x)
-    (px, ldx), (py, ldy) = _activation("x", x, x), _activation("y", y, x)
-    pg, pb, pm, pr = _statistics(M, E, gamma=gamma, beta=beta, mean=mean, rstd=rstd)
-    _here(stream, x, gamma, beta, y, mean, rstd)
-    _raise(lib().helix_layer_norm_fwd(px, ldx, pg, pb, py, ldy, pm, pr, M, E, kind, float(eps), _stream(stream)), "helix_layer_norm_fwd")
+    dev = _current(x, stream)
+    shape, dtype = _rows("x", x)
+    M, E = shape
+    px, ldx = _activation("x", x, shape, dtype, dev)
+    py, ldy = _activation("y", y, shape, dtype, dev)
+    _raise(lib().helix_layer_norm_fwd(px, ldx, _vector("gamma", gamma, E, dev), _vector("beta", beta, E, dev), py, ldy,
+                                      None if mean is None else _vector("mean", mean, M, dev), None if rstd is None else _vector("rstd", rstd, M, dev),
+                                      M, E, _TYPES[dtype], float(eps), _stream(stream)), "helix_layer_norm_fwd")
 
 
 def helix_layer_norm_bwd_workspace_bytes(M, E) -> int:
@@ -417,36 +429,47 @@ def helix_layer_norm_bwd_workspace_bytes(M, E) -> int:
 def helix_layer_norm_bwd(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, workspace, stream=None):
     """dx[M,E], dgamma[E], dbeta[E] <- gradients of helix_layer_norm_fwd; workspace: uint8 CUDA tensor of
     helix_layer_norm_bwd_workspace_bytes(M, E) bytes."""
-    M, E, kind = _rows("x", x)
-    (pdy, lddy), (px, ldx), (pdx, lddx) = _activation("dy", dy, x), _activation("x", x, x), _activation("dx", dx, x)
-    pg, pm, pr, pdg, pdb = _statistics(M, E, gamma=gamma, mean=mean, rstd=rstd, dgamma=dgamma, dbeta=dbeta)
-    pw, nw = _workspace(workspace)
-    _here(stream, dy, x, gamma, mean, rstd, dx, dgamma, dbeta, workspace)
-    _raise(lib().helix_layer_norm_bwd(pdy, lddy, px, ldx, pg, pm, pr, pdx, lddx, pdg, pdb, pw, nw, M, E, kind, _stream(stream)), "helix_layer_norm_bwd")
+    dev = _current(x, stream)
+    shape, dtype = _rows("x", x)
+    M, E = shape
+    pdy, lddy = _activation("dy", dy, shape, dtype, dev)
+    px, ldx = _activation("x", x, shape, dtype, dev)
+    pdx, lddx = _activation("dx", dx, shape, dtype, dev)
+    pw, nw = _workspace(workspace, dev)
+    _raise(lib().helix_layer_norm_bwd(pdy, lddy, px, ldx, _vector("gamma", gamma, E, dev), _vector("mean", mean, M, dev), _vector("rstd", rstd, M, dev), pdx, lddx,
+                                      _vector("dgamma", dgamma, E, dev), _vector("dbeta", dbeta, E, dev), pw, nw, M, E, _TYPES[dtype], _stream(stream)),
+           "helix_layer_norm_bwd")
 
 
 def helix_dropout_add_layer_norm_fwd(x, residual, s, gamma, beta, y, mean, rstd, p, rng, eps=1e-5, first_row=0, stream=None):
     """s <- residual + dropout(x), y, mean, rstd <- layer norm of s (see helix_dropout_add_fwd and helix_layer_norm_fwd)."""
-    M, E, kind = _rows("x", x)
-    (px, ldx), (pr, ldr), (ps, lds), (py, ldy) = (_activation(n, t, x) for n, t in (("x", x), ("residual", residual), ("s", s), ("y", y)))
-    pg, pb, pm, pd = _statistics(M, E, gamma=gamma, beta=beta, mean=mean, rstd=rstd)
-    pn = _generator(rng)
-    _here(stream, x, residual, s, gamma, beta, y, mean, rstd, rng)
-    _raise(lib().helix_dropout_add_layer_norm_fwd(px, ldx, pr, ldr, ps, lds, pg, pb, py, ldy, pm, pd, M, E, kind, float(p), pn, int(first_row),
-                                                  float(eps), _stream(stream)), "helix_dropout_add_layer_norm_fwd")
+    dev = _current(x, stream)
+    shape, dtype = _rows("x", x)
+    M, E = shape
+    px, ldx = _activation("x", x, shape, dtype, dev)
+    pr, ldr = _activation("residual", residual, shape, dtype, dev)
+    ps, lds = _activation("s", s, shape, dtype, dev)
+    py, ldy = _activation("y", y, shape, dtype, dev)
+    _raise(lib().helix_dropout_add_layer_norm_fwd(px, ldx, pr, ldr, ps, lds, _vector("gamma", gamma, E, dev), _vector("beta", beta, E, dev), py, ldy,
+                                                  None if mean is None else _vector("mean", mean, M, dev), None if rstd is None else _vector("rstd", rstd, M, dev),
+                                                  M, E, _TYPES[dtype], float(p), _generator(rng, dev), int(first_row), float(eps), _stream(stream)), "helix_dropout_add_layer_norm_fwd")
 
 
 def helix_dropout_add_layer_norm_bwd(dy, ds, s, gamma, mean, rstd, dx, dresidual, dgamma, dbeta, workspace, p, rng, first_row=0, stream=None):
     """dresidual <- ds + gradient of the layer norm of s, dx <- its dropped-out share, dgamma, dbeta.  ds may be None."""
-    M, E, kind = _rows("s", s)
-    (pdy, lddy), (ps, lds), (pdx, lddx), (pdr, lddr) = (_activation(n, t, s) for n, t in (("dy", dy), ("s", s), ("dx", dx), ("dresidual", dresidual)))
-    pds, ldds = (None, 0) if ds is None else _activation("ds", ds, s)
-    pg, pm, pr, pdg, pdb = _statistics(M, E, gamma=gamma, mean=mean, rstd=rstd, dgamma=dgamma, dbeta=dbeta)
-    pw, nw = _workspace(workspace)
-    pn = _generator(rng)
-    _here(stream, dy, ds, s, gamma, mean, rstd, dx, dresidual, dgamma, dbeta, workspace, rng)
-    _raise(lib().helix_dropout_add_layer_norm_bwd(pdy, lddy, pds, ldds, ps, lds, pg, pm, pr, pdx, lddx, pdr, lddr, pdg, pdb, pw, nw, M, E, kind, float(p),
-                                                  pn, int(first_row), _stream(stream)), "helix_dropout_add_layer_norm_bwd")
+    dev = _current(s, stream)
+    shape, dtype = _rows("s", s)
+    M, E = shape
+    pdy, lddy = _activation("dy", dy, shape, dtype, dev)
+    pds, ldds = (None, 0) if ds is None else _activation("ds", ds, shape, dtype, dev)
+    ps, lds = _activation("s", s, shape, dtype, dev)
+    pdx, lddx = _activation("dx", dx, shape, dtype, dev)
+    pdr, lddr = _activation("dresidual", dresidual, shape, dtype, dev)
+    pw, nw = _workspace(workspace, dev)
+    _raise(lib().helix_dropout_add_layer_norm_bwd(pdy, lddy, pds, ldds, ps, lds, _vector("gamma", gamma, E, dev), _vector("mean", mean, M, dev),
+                                                  _vector("rstd", rstd, M, dev), pdx, lddx, pdr, lddr, _vector("dgamma", dgamma, E, dev),
+                                                  _vector("dbeta", dbeta, E, dev), pw, nw, M, E, _TYPES[dtype], float(p), _generator(rng, dev), int(first_row),
+                                                  _stream(stream)), "helix_dropout_add_layer_norm_bwd")
 
 
 # ---------------------------------------------------------------- gated feed-forward projections
@@ -459,21 +482,17 @@ def _gated(a, w, activation):
         raise ValueError(f"activation: need one of {tuple(_ACTIVATIONS)}")
     if a.dim() != 2 or w.dim() != 2 or w.shape[1] % 2:
         raise ValueError("need matrices a [M, K] and w [K, 2F]")
-    return a.shape[0], a.shape[1], w.shape[1] // 2, _ACTIVATIONS[activation]
-
-
-def _tall(name, t, rows, cols):
-    """_matrix, where the pitch of a single row counts for nothing."""
-    ptr, ld = _matrix(name, t, rows, cols)
-    return ptr, ld if rows > 1 else cols
+    return *a.shape, w.shape[1] // 2, _ACTIVATIONS[activation]
 
 
 def helix_gated_linear_fwd(a, w, h, gu=None, activation="silu", stream=None):
     """h[M,F] <- act(a @ w[:, :F]) * (a @ w[:, F:]); gu[M,2F], if given, <- a @ w for the backward.  bf16, 2-D views with contiguous rows."""
     M, K, F, act = _gated(a, w, activation)
-    (pa, lda), (pw, ldw), (ph, ldh) = _tall("a", a, M, K), _matrix("w", w, K, 2 * F), _tall("h", h, M, F)
-    pg, ldg = (None, 0) if gu is None else _tall("gu", gu, M, 2 * F)
-    _here(stream, a, w, h, gu)
+    dev = _current(a, stream)
+    pa, lda = _activation("a", a, (M, K), _BF16, dev)
+    pw, ldw = _activation("w", w, (K, 2 * F), _BF16, dev)
+    pg, ldg = (None, 0) if gu is None else _activation("gu", gu, (M, 2 * F), _BF16, dev)
+    ph, ldh = _activation("h", h, (M, F), _BF16, dev)
     _raise(lib().helix_gated_linear_fwd(pa, lda, pw, ldw, pg, ldg, ph, ldh, M, K, F, act, _stream(stream)), "helix_gated_linear_fwd")
 
 
@@ -485,9 +504,12 @@ def helix_gated_linear_bwd(a, w, dh, da, dw, workspace, gu=None, activation="sil
     """da[M,K], dw[K,2F] <- gradients of helix_gated_linear_fwd for dh[M,F], from the gu it wrote or, without, from a and w alone; workspace:
     uint8 CUDA tensor of helix_gated_linear_bwd_workspace_bytes(M, K, F) bytes."""
     M, K, F, act = _gated(a, w, activation)
-    (pa, lda), (pw, ldw), (ph, ldh) = _tall("a", a, M, K), _matrix("w", w, K, 2 * F), _tall("dh", dh, M, F)
-    (pda, ldda), (pdw, lddw) = _tall("da", da, M, K), _matrix("dw", dw, K, 2 * F)
-    pg, ldg = (None, 0) if gu is None else _tall("gu", gu, M, 2 * F)
-    pws, nws = _workspace(workspace)
-    _here(stream, a, w, dh, da, dw, gu, workspace)
+    dev = _current(a, stream)
+    pa, lda = _activation("a", a, (M, K), _BF16, dev)
+    pw, ldw = _activation("w", w, (K, 2 * F), _BF16, dev)
+    pg, ldg = (None, 0) if gu is None else _activation("gu", gu, (M, 2 * F), _BF16, dev)
+    ph, ldh = _activation("dh", dh, (M, F), _BF16, dev)
+    pda, ldda = _activation("da", da, (M, K), _BF16, dev)
+    pdw, lddw = _activation("dw", dw, (K, 2 * F), _BF16, dev)
+    pws, nws = _workspace(workspace, dev)
     _raise(lib().helix_gated_linear_bwd(pa, lda, pw, ldw, pg, ldg, ph, ldh, pda, ldda, pdw, lddw, pws, nws, M, K, F, act, _stream(stream)), "helix_gated_linear_bwd")

@@ -333,6 +333,21 @@ inline TilePair linear_gradient_tiles(int M, int K, int N, int parts) {
   return TilePair{(TileKind)best->input, (TileKind)best->weight};
 }
 
+// The gated backward's input gradient: [M][N] times [N][K] with N = 2F, a long contraction and often few tiles, which the models above, fitted to N up
+// to 24 x 128, do not know.  Where it is long its contraction is cut into parts that fill the chip, in a launch of its own.
+// Whole / in parts, us of the backward from kept projections, M x K x F: 1 x 2048 x 5504 60 / 31; 1 x 4096 x 11008 149 / 110; 32 x 1024 x 8192 52 / 31; 300 x 4096 x 4096
+// 120 / 87; 700 x 2048 x 5504 172 / 128; 700 x 512 x 9984 117 / 78; 2000 x 1024 x 5504 184 / 144; 4000 x 512 x 8000 290 / 238; 6000 x 640 x 9984 517 / 516; 8000 x 512 x
+// 5504 340 / 357; 8 x 5120 x 1728 21 / 27; 100 x 1024 x 2752 22.9 / 24.6; 300 x 1024 x 1024 13 / 21.
+inline TileKind split_input_tile(int M) { return M <= 64 ? TileKind::k64 : TileKind::k128; }
+inline int split_input_parts(int M, int K, int N) {
+  const int e = tile_edge(split_input_tile(M));
+  const long long tiles = (long long)((M + e - 1) / e) * ((K + e - 1) / e);
+  if (M > 4096 || N < 6144 || tiles >= 512) return 1;
+  return (int)std::min<long long>(std::min<long long>((512 + tiles - 1) / tiles, N / 256), 32);
+}
+
+// The gated projections of few rows (skinny.hip; on tiles / so, us: 1 x 2048 x 5504 12.5 / 11.5, 8 x 5120 x 1728 25.9 / 18.9, 32 x 1024 x 8192 9.6 / 9.4, 1 x 4096 x 11008 36.2 / 37.5).
+inline bool gated_skinny(int M) { return M <= 32; }
 // The gated projections: tiles of h of 256 x 128, 128 x 64 and 64 x 64 elements.
 inline TileKind gated_tile(int M, int K, int F) {
   (void)K;

@@ -9,6 +9,7 @@
 // into dg and du (recomputation: 4MKF FLOPs more, 2F elements a token less to keep).  da and dw are then the linear layer's two gradient products.
 //
 // dg and du are rounded to bf16, the type in which the matrix pipes take them; sums are fp32; dw is rounded to the weights' type once, from the whole fp32 sum.
+#include "gated_math.hpp"
 #include "gemm.hpp"
 #include "helix_common.hpp"
 #include "kernels.hpp"
@@ -43,19 +44,37 @@ struct GatedBlocks {
   }
 };
 
-// The activation and its derivative.
-template <Activation ACT>
-__device__ __forceinline__ void activate(float g, float& value, float& slope) {
-  if constexpr (ACT == Activation::silu) {   // s = 1 / (1 + e^-g):  g s,  s (1 + g (1 - s))
-    const float s = __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-kLog2e * g));
-    value = g * s;
-    slope = s * fmaf(g, 1.f - s, 1.f);
-  } else {                                   // P(g) the normal distribution:  g P,  P + g P'
-    const float P = fmaf(0.5f, erff(g * 0.70710678f), 0.5f);
-    value = g * P;
-    slope = fmaf(g * 0.39894228f, __builtin_amdgcn_exp2f(-0.5f * kLog2e * g * g), P);
+// A wave's part of dh, 32 * BI rows x 32 * BH columns, in registers: requested when the last copies are out, so that it is there when the sums are.  A lane loads
+// 16 bytes at a time of the row that its sums belong to, those of the lane 32 further on in between.
+template <int BI, int BH>
+struct Gradient {
+  static constexpr int IN_FLIGHT = BI * BH * 2;
+  const __bf16* base;   // column of the wave's first block
+  long long ld;
+  int i_wave, M, lane;
+  u32x4 piece[BI][BH][2];
+  __device__ __forceinline__ void operator()() {
+#pragma unroll
+    for (int ib = 0; ib < BI; ib++) {
+      const int i = i_wave + 32 * ib + (lane & 31);
+      const __bf16* const row = base + (size_t)(i < M ? i : M - 1) * ld + 8 * (lane >> 5);
+#pragma unroll
+      for (int jb = 0; jb < BH; jb++)
+#pragma unroll
+        for (int q = 0; q < 2; q++) piece[ib][jb][q] = *reinterpret_cast<const u32x4*>(row + 32 * jb + 16 * q);
+    }
   }
-}
+  // the four columns 8 g + 4 (lane / 32) .. of a block
+  __device__ __forceinline__ void columns(int ib, int jb, int g, float (&d)[4]) const {
+    const u32x4& x = piece[ib][jb][g >> 1];
+    const auto a = __builtin_amdgcn_permlane32_swap(x[0], x[2], false, false), b = __builtin_amdgcn_permlane32_swap(x[1], x[3], false, false);
+    const uint32_t lo = a[g & 1], hi = b[g & 1];
+    d[0] = __uint_as_float(lo << 16);
+    d[1] = __uint_as_float(lo & 0xffff0000u);
+    d[2] = __uint_as_float(hi << 16);
+    d[3] = __uint_as_float(hi & 0xffff0000u);
+  }
+};
 
 // GRAD: dgu <- [dg du] from a, w and dh (rows up to a multiple of 32, zeros behind row M); else h, and gu = [g u] unless null.
 template <typename G, bool GRAD, Activation ACT>
@@ -78,7 +97,10 @@ __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_e
   XOp xsrc((const __bf16*)p.a, p.lda, i0, p.M, 0, lane, w);
   YOp ysrc((const __bf16*)p.w, p.ldw, j0, p.F, lane, w);
   f32x16 acc[BJ][BI];
-  gemm_sums<G, XOp, YOp, GatedBlocks<G::TJ>, false>(xsrc, ysrc, p.K / G::STEP, base, lane, w, acc);
+  const int i_wave = i0 + 32 * BI * (w & 1), j_wave = j0 + W * (w >> 1);
+  Gradient<BI, BH> dh = {(const __bf16*)p.dh + (j_wave < p.F ? j_wave : 0), p.lddh, i_wave, p.M, lane, {}};
+  if constexpr (GRAD) gemm_sums<G, XOp, YOp, GatedBlocks<G::TJ>, false>(xsrc, ysrc, p.K / G::STEP, base, lane, w, acc, 0, 0, dh);
+  else gemm_sums<G, XOp, YOp, GatedBlocks<G::TJ>, false>(xsrc, ysrc, p.K / G::STEP, base, lane, w, acc);
 
   if constexpr (BI * BJ == 16) {   // see gemm_block
 #pragma unroll
@@ -86,7 +108,6 @@ __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_e
 #pragma unroll
       for (int ib = 0; ib < BI; ib++) asm volatile("" : "+a"(acc[jb][ib]));
   }
-  const int i_wave = i0 + 32 * BI * (w & 1), j_wave = j0 + W * (w >> 1);
   constexpr int PIECE = 32 * W * 2;   // bytes of 32 rows
   if constexpr (!GRAD) {
     char* const out = smem + w * PIECE;
@@ -121,34 +142,25 @@ __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_e
       __builtin_amdgcn_sched_barrier(0);
     }
   } else {
-    // this wave's part of dh, as whole rows
     const int rows = (p.M + 31) & ~31;
-    const uint32_t dh_lds = base + w * (BI * PIECE);
-    char* const out = smem + kWaves * BI * PIECE + w * (2 * PIECE);
-    const __bf16* const dh = (const __bf16*)p.dh + (j_wave < p.F ? j_wave : 0);
-    const TileLoader<W, 32, 1> load(lane, 0, (int)p.lddh);
+    char* const out = smem + w * (2 * PIECE);
 #pragma unroll
     for (int ib = 0; ib < BI; ib++) {
       const int i = i_wave + 32 * ib;
-      load.issue(dh, i < p.M ? i : p.M - 1, p.M, dh_lds + ib * PIECE);
-    }
-    wait_tile_loads();
-#pragma unroll
-    for (int ib = 0; ib < BI; ib++) {
-      const int i = i_wave + 32 * ib;
-      const bool exists = i + (lane & 31) < p.M;
+      const uint32_t exists = i + (lane & 31) < p.M ? ~0u : 0u;   // a mask and no condition, which would be a branch for every element
 #pragma unroll
       for (int jb = 0; jb < BH; jb++) {
         f32x16 dg, du;
 #pragma unroll
         for (int q = 0; q < 4; q++) {
-          const bf16x4 d = *reinterpret_cast<const bf16x4*>(smem + w * (BI * PIECE) + ib * PIECE + lds_chunk_off<W>(lane & 31, 4 * jb + q) + 8 * (lane >> 5));
+          float d[4];
+          dh.columns(ib, jb, q, d);
 #pragma unroll
           for (int e = 0; e < 4; e++) {
             float value, slope;
             activate<ACT>(acc[jb][ib][4 * q + e], value, slope);
-            dg[4 * q + e] = exists ? (float)d[e] * acc[BH + jb][ib][4 * q + e] * slope : 0.f;
-            du[4 * q + e] = exists ? (float)d[e] * value : 0.f;
+            dg[4 * q + e] = __uint_as_float(__float_as_uint(d[e] * acc[BH + jb][ib][4 * q + e] * slope) & exists);
+            du[4 * q + e] = __uint_as_float(__float_as_uint(d[e] * value) & exists);
           }
         }
         helix::put_rows<W>(out, lane, jb, dg);
@@ -210,6 +222,7 @@ hipError_t launch_tiles(const Gated& p, hipStream_t stream) {
 }
 template <bool GRAD, Activation ACT>
 hipError_t launch_projections(const Gated& p, hipStream_t stream) {
+  if (gated_skinny(p.M)) return launch_skinny_projections(p, GRAD, ACT, stream);
   switch (gated_tile(p.M, p.K, p.F)) {
     case TileKind::k256: return launch_tiles<Wide, GRAD, ACT>(p, stream);
     case TileKind::k128: return launch_tiles<Middle, GRAD, ACT>(p, stream);
@@ -232,7 +245,7 @@ hipError_t launch_gated_fwd(const Gated& p, Activation act, hipStream_t stream) 
 }
 
 // Workspace: that of the linear layer's backward with 2F columns, then dgu.
-size_t gated_bwd_products_bytes(int M, int K, int F) { return (linear_bwd_workspace_bytes(M, K, 2 * F) + 255) & ~(size_t)255; }
+size_t gated_bwd_products_bytes(int M, int K, int F) { return (linear_bwd_ragged_workspace_bytes(M, K, 2 * F) + 255) & ~(size_t)255; }
 size_t gated_bwd_workspace_bytes(int M, int K, int F) { return gated_bwd_products_bytes(M, K, F) + (size_t)((M + 31) & ~31) * 2 * F * 2; }
 
 hipError_t launch_gated_bwd(const Gated& given, const void* gu, long long ldgu, void* da, long long ldda, void* dw, long long lddw, void* workspace, Activation act,

@@ -209,9 +209,16 @@ struct BlocksSideBySide {
   __device__ __forceinline__ static constexpr int column(int BJ, int wj, int b) { return 32 * (BJ * wj + b); }
 };
 
+// What a wave asks of memory when the last copies of its stages are out: IN_FLIGHT loads that nothing waits for before the sums are complete.
+struct NothingBeforeTheEnd {
+  static constexpr int IN_FLIGHT = 0;
+  __device__ __forceinline__ void operator()() const {}
+};
+
 // The sums of a wave over nk stages.  RAGGED: the last stage of X (stored by rows of the contraction index, `ldx` elements apart) ends with its row `last`.
-template <typename G, typename XOp, typename YOp, typename YBlocks, bool RAGGED>
-__device__ __forceinline__ void gemm_sums(XOp& xsrc, YOp& ysrc, int nk, uint32_t base, int lane, int w, f32x16 (&acc)[G::BJ][G::BI], long long ldx = 0, int last = 0) {
+template <typename G, typename XOp, typename YOp, typename YBlocks, bool RAGGED, typename Before = NothingBeforeTheEnd>
+__device__ __forceinline__ void gemm_sums(XOp& xsrc, YOp& ysrc, int nk, uint32_t base, int lane, int w, f32x16 (&acc)[G::BJ][G::BI], long long ldx = 0, int last = 0,
+                                          Before&& before_the_end = Before()) {
   constexpr int BI = G::BI, BJ = G::BJ, NS = G::STEP / 16, AHEAD = G::AHEAD, NST = G::NST, STAGE = G::STAGE;
   const int wi = w & 1, wj = w >> 1;
   constexpr int NDMA = XOp::DMA + YOp::DMA;
@@ -323,9 +330,10 @@ __device__ __forceinline__ void gemm_sums(XOp& xsrc, YOp& ysrc, int nk, uint32_t
     stage(std::true_type{}, std::true_type{});
     stage_barrier<(AHEAD - 2) * NDMA>();
   }
+  before_the_end();
   for (; k < (STAGE_AHEAD ? nk - 1 : nk); k++) {
     stage(std::false_type{}, std::true_type{});
-    stage_barrier<0>();
+    stage_barrier<std::remove_reference<Before>::type::IN_FLIGHT>();
   }
   // The last stage has nothing to read ahead and, as the tile leaves from the registers, nobody to wait for: its reads held up the workgroup beside this one (forward of
   // 12480 x 128 x 128 3.39 -> 3.27 us, 4256 x 512 x 256 4.91 -> 4.84).

@@ -74,6 +74,7 @@ hipError_t launch_linear_bwd(const void* a, long long lda, const void* w, long l
                              long long ldda, float* dw, long long lddw, void* workspace, int M, int K, int N, hipStream_t stream);
 
 // The same two products for any M and a bf16 weight gradient (gated.hip); dout has rows of zeros up to the next multiple of 32.
+size_t linear_bwd_ragged_workspace_bytes(int M, int K, int N);
 hipError_t launch_linear_bwd_ragged(const void* a, long long lda, const void* w, long long ldw, const void* dout, long long ldd, void* da,
                                     long long ldda, void* dw, long long lddw, void* workspace, int M, int K, int N, hipStream_t stream);
 
@@ -124,6 +125,8 @@ struct Gated {
   long long lda, ldw, lddh, ldh, ldgu;
   int M, K, F;
 };
+// At most 32 rows (skinny.hip); grad: dgu in gu, as gated_kernel makes it.
+hipError_t launch_skinny_projections(const Gated& p, bool grad, Activation act, hipStream_t stream);
 hipError_t launch_gated_fwd(const Gated& p, Activation act, hipStream_t stream);
 size_t gated_bwd_workspace_bytes(int M, int K, int F);
 // gu: what the forward kept, or null: the projections are computed again.  dw is bf16.

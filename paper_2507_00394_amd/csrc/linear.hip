@@ -112,6 +112,12 @@ size_t linear_bwd_workspace_bytes(int M, int K, int N) {
   return linear_bwd_wt_bytes(K, N) + (parts > 1 ? (size_t)parts * K * N * sizeof(float) : 0);
 }
 
+// With the input gradient in parts (linear_bwd with RAGGED only): the slabs hold either's partial results.
+size_t linear_bwd_ragged_workspace_bytes(int M, int K, int N) {
+  const int parts = linear_bwd_weight_parts(M, K, N), input_parts = split_input_parts(M, K, N);
+  return linear_bwd_wt_bytes(K, N) + std::max(parts > 1 ? (size_t)parts * K * N * sizeof(float) : 0, input_parts > 1 ? (size_t)input_parts * M * K * sizeof(float) : 0);
+}
+
 // Input gradient da = dout * w^T.  With w as stored ([K][N], contraction index n contiguous) both
 // operands would reach LDS in 64-byte row pieces, the least efficient pattern of the copy path
 // (measured 30 % slower than the forward product); on the large tile a transposed copy of the small weight matrix
@@ -135,6 +141,17 @@ static hipError_t launch_products(TilePair kind, const Gemm<__bf16>& in, const G
                                        : launch_gradients<Tile64, false, Tile64ShortStages, RAGGED>(in, grad_w, stream);
 }
 
+template <bool RAGGED, typename WeightT>
+static hipError_t launch_weight(TileKind kind, const Gemm<WeightT>& grad_w, hipStream_t stream) {
+  return kind == TileKind::k256 ? launch_gemm_tile<Tile256, true, true, RAGGED>(grad_w, stream) : launch_gemm_tile<Tile128, true, true, RAGGED>(grad_w, stream);
+}
+template <typename T>
+static hipError_t launch_sum_parts(const float* slabs, T* dst, long long ld_dst, int rows, int cols, int parts, hipStream_t stream) {
+  const long long quads = (long long)rows * cols / 4;
+  hipLaunchKernelGGL(sum_parts_kernel<T>, dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, stream, slabs, dst, ld_dst, rows, cols, parts);
+  return hipGetLastError();
+}
+
 // RAGGED: any M; dout then has rows of zeros up to the next multiple of 32.
 template <bool RAGGED, typename WeightT>
 static hipError_t linear_bwd(const void* a, long long lda, const void* w, long long ldw, const void* dout, long long ldd, void* da, long long ldda, WeightT* dw,
@@ -144,8 +161,15 @@ static hipError_t linear_bwd(const void* a, long long lda, const void* w, long l
   const int parts = linear_bwd_weight_parts(M, K, N);
   const int per = parts == 1 ? M : (((M + 31) / 32 + parts - 1) / parts) * 32;    // tokens per part, a multiple of the stage length
   Gemm<__bf16> in = {(const __bf16*)dout, (const __bf16*)w, (__bf16*)da, ldd, ldw, ldda, 0, M, K, N, 0, 0, 1, N, 1};
-  const TilePair kind = linear_gradient_tiles(M, K, N, parts);
-  if (kind.input == TileKind::k256) {
+  TilePair kind = linear_gradient_tiles(M, K, N, parts);
+  const int input_parts = RAGGED ? split_input_parts(M, K, N) : 1;
+  if (input_parts > 1) {   // the input gradient's contraction in parts too, whose sums come before the weight gradient takes the slabs
+    const int per_in = (N / 64 + input_parts - 1) / input_parts * 64;
+    const Gemm<float> in_parts = {(const __bf16*)dout, (const __bf16*)w, slabs, ldd, ldw, K, (long long)M * K, M, K, N, 0, 0, (N + per_in - 1) / per_in, per_in, 1};
+    hipError_t e = split_input_tile(M) == TileKind::k64 ? launch_gemm_tile<Tile64, false, false>(in_parts, stream) : launch_gemm_tile<Tile128, false, false>(in_parts, stream);
+    if (e != hipSuccess) return e;
+    if ((e = launch_sum_parts(slabs, (__bf16*)da, ldda, M, K, in_parts.parts, stream)) != hipSuccess) return e;
+  } else if (kind.input == TileKind::k256) {
     hipLaunchKernelGGL(transpose_kernel, dim3((unsigned)(N / 64), (unsigned)(K / 64)), dim3(256), 0, stream, (const __bf16*)w, ldw, wt, (long long)K);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
@@ -154,14 +178,11 @@ static hipError_t linear_bwd(const void* a, long long lda, const void* w, long l
   }
   if (parts == 1) {
     const Gemm<WeightT> grad_w = {(const __bf16*)a, (const __bf16*)dout, dw, lda, ldd, lddw, 0, K, N, M, 0, 0, 1, per, side};
-    return launch_products<RAGGED>(kind, in, grad_w, stream);
+    return input_parts > 1 ? launch_weight<RAGGED>(kind.weight, grad_w, stream) : launch_products<RAGGED>(kind, in, grad_w, stream);
   }
   const Gemm<float> grad_w = {(const __bf16*)a, (const __bf16*)dout, slabs, lda, ldd, N, (long long)K * N, K, N, M, 0, 0, parts, per, side};
-  const hipError_t e = launch_products<RAGGED>(kind, in, grad_w, stream);
-  if (e != hipSuccess) return e;
-  const long long quads = (long long)K * N / 4;
-  hipLaunchKernelGGL(sum_parts_kernel<WeightT>, dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, stream, slabs, dw, lddw, K, N, parts);
-  return hipGetLastError();
+  const hipError_t e = input_parts > 1 ? launch_weight<RAGGED>(kind.weight, grad_w, stream) : launch_products<RAGGED>(kind, in, grad_w, stream);
+  return e != hipSuccess ? e : launch_sum_parts(slabs, dw, lddw, K, N, parts, stream);
 }
 
 hipError_t launch_linear_bwd(const void* a, long long lda, const void* w, long long ldw, const void* dout, long long ldd, void* da,
