@@ -346,13 +346,34 @@ inline int split_input_parts(int M, int K, int N) {
   return (int)std::min<long long>(std::min<long long>((512 + tiles - 1) / tiles, N / 256), 32);
 }
 
+// Its weight gradient: parts until the 256 x 256 tiles fill half of the chip; the input gradient's workgroups, which share the launch, fill the rest, and every part less is a
+// slab of fp32 sums less to write and read.  Until they fill it twice, as above / once / half / a quarter, us of the backward from kept projections: 20000 x 1024 x
+// 2752 564 / 537 / 483 / 532; 16384 x 4096 x 1408 720 / 700 / 660 / 667; 32000 x 512 x 5504 1033 / 1102 / 972 / 1008; 8192 x 1024 x 1024 - / - / 91 / 102; 30000 x 384 x 384 - / - / 81.0 /
+// 81.3.
+inline int split_weight_parts(int M, int K, int N) {
+  const int tiles = ((K + 255) / 256) * ((N + 255) / 256);
+  return std::min(linear_bwd_weight_parts(M, K, N), (128 + tiles - 1) / tiles);
+}
+
 // The gated projections of few rows (skinny.hip; on tiles / so, us: 1 x 2048 x 5504 12.5 / 11.5, 8 x 5120 x 1728 25.9 / 18.9, 32 x 1024 x 8192 9.6 / 9.4, 1 x 4096 x 11008 36.2 / 37.5).
 inline bool gated_skinny(int M) { return M <= 32; }
-// The gated projections: tiles of h of 256 x 128, 128 x 64 and 64 x 64 elements.
+// The gated projections' tiles: 256 x 128, 128 x 64 and 64 x 64 elements of h, twice as many columns of the product.  Time models as those of linear_tile, fitted to 97 shapes (33 to
+// 30000 tokens, K to 5120, F to 11008): us per 1000 contraction indices with the chip full and alone, for the start and end of a round and of the last one, per MB of h, per MB
+// read (the weights by every XCD).
+// 256 / 128 / 64, us, M x K x F: 300 x 4096 x 4096 75.3 / 30.0 / 38.0; 103 x 2816 x 8000 54.1 / 22.6 / 17.9; 2077 x 5120 x 1728 93.5 / 87.0 / 104; 26016 x 3456 x 320 160 / 139 / 179;
+// 20166 x 4096 x 384 109 / 147 / 188; 5097 x 256 x 3584 37.6 / 28.8 / 34.7; 16384 x 4096 x 1408 305 / 381 / 489; 700 x 2048 x 5504 42.9 / 47.6 / 45.9.
+// 0.1 % off the fastest tile, at worst 1.07 times its time (the last of these).
 inline TileKind gated_tile(int M, int K, int F) {
-  (void)K;
-  const long long wide = (long long)((M + 255) / 256) * ((F + 127) / 128), middle = (long long)((M + 127) / 128) * ((F + 63) / 64);
-  return wide >= 256 ? TileKind::k256 : middle >= 256 ? TileKind::k128 : TileKind::k64;
+  struct Cost { int rows, cols; double full, alone, round, last, mb_written, mb_read; };
+  static constexpr Cost cost[3] = {{256, 128, 23.4, 15.6, 6.18, 7.58, .0229, 0}, {128, 64, 16.4, 5.84, 0, 3.43, .185, .0077}, {64, 64, 10.3, 4.43, .373, 2.99, .139, .0078}};
+  const double k = K * 1e-3, written = (double)M * F * 2e-6, read = ((double)M * K + 16. * K * F) * 2e-6;
+  double t[3];
+  for (int i = 0; i < 3; i++) {
+    const Cost& c = cost[i];
+    const double n = 8 * std::ceil(((M + c.rows - 1) / c.rows) * (double)((F + c.cols - 1) / c.cols) / 8), slots = tile_slots((TileKind)i), rounds = std::ceil(n / slots) - 1;
+    t[i] = rounds * (c.full * k + c.round) + (c.alone + (c.full - c.alone) * pace((TileKind)i, n - rounds * slots)) * k + c.last + c.mb_written * written + c.mb_read * read;
+  }
+  return (TileKind)(std::min_element(t, t + 3) - t);
 }
 
 // ---------------------------------------------------------------- layer norm's rows

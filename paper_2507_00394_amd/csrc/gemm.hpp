@@ -152,8 +152,8 @@ __device__ __forceinline__ void store_block(float* row, int half, const f32x16& 
 __device__ __forceinline__ void store_block(__bf16* row, int half, const f32x16& acc) {
   for_each_chunk(half, acc, [&](int chunk, const u32x4& x) __attribute__((always_inline)) { *reinterpret_cast<u32x4*>(row + 8 * chunk) = x; });
 }
-// Stores the tile; `rows` of its rows and `cols` of its columns (a multiple of 32) exist.
-template <int W, typename T>
+// Stores the tile; `rows` of its rows and `cols` of its columns (a multiple of 32) exist.  ONCE: the caches need not keep them.
+template <int W, bool ONCE = false, typename T>
 __device__ __forceinline__ void store_rows(const char* tile, int lane, T* row0, long long row_stride, int rows, int cols) {
   constexpr int PER_CHUNK = 16 / sizeof(T), CH = W / PER_CHUNK, PER = 64 / CH;   // elements of a chunk, chunks of a row, rows of a piece
   pin(lane);
@@ -165,7 +165,10 @@ __device__ __forceinline__ void store_rows(const char* tile, int lane, T* row0, 
     const int off = sizeof(T) == 4 ? float_chunk_off<W>(r, chunk) : lds_chunk_off<W>(r, chunk);
     const u32x4 x = *reinterpret_cast<const u32x4*>(tile + off);
     char* const rows_i = const_cast<char*>(uniform_ptr(reinterpret_cast<const char*>(row0 + (size_t)(i * PER) * row_stride)));
-    if (r < rows && chunk * PER_CHUNK < cols) *reinterpret_cast<u32x4*>(rows_i + lane_off) = x;
+    if (r < rows && chunk * PER_CHUNK < cols) {
+      if constexpr (ONCE) __builtin_nontemporal_store(x, reinterpret_cast<u32x4*>(rows_i + lane_off));
+      else *reinterpret_cast<u32x4*>(rows_i + lane_off) = x;
+    }
   }
 }
 // All but the N newest vector memory operations of this wave are done, and every wave of the workgroup has got here.

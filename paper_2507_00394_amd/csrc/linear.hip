@@ -114,7 +114,7 @@ size_t linear_bwd_workspace_bytes(int M, int K, int N) {
 
 // With the input gradient in parts (linear_bwd with RAGGED only): the slabs hold either's partial results.
 size_t linear_bwd_ragged_workspace_bytes(int M, int K, int N) {
-  const int parts = linear_bwd_weight_parts(M, K, N), input_parts = split_input_parts(M, K, N);
+  const int parts = split_weight_parts(M, K, N), input_parts = split_input_parts(M, K, N);
   return linear_bwd_wt_bytes(K, N) + std::max(parts > 1 ? (size_t)parts * K * N * sizeof(float) : 0, input_parts > 1 ? (size_t)input_parts * M * K * sizeof(float) : 0);
 }
 
@@ -158,7 +158,7 @@ static hipError_t linear_bwd(const void* a, long long lda, const void* w, long l
                              long long lddw, void* workspace, int M, int K, int N, int side, hipStream_t stream) {
   __bf16* const wt = (__bf16*)workspace;
   float* const slabs = reinterpret_cast<float*>(static_cast<char*>(workspace) + linear_bwd_wt_bytes(K, N));
-  const int parts = linear_bwd_weight_parts(M, K, N);
+  const int parts = RAGGED ? split_weight_parts(M, K, N) : linear_bwd_weight_parts(M, K, N);
   const int per = parts == 1 ? M : (((M + 31) / 32 + parts - 1) / parts) * 32;    // tokens per part, a multiple of the stage length
   Gemm<__bf16> in = {(const __bf16*)dout, (const __bf16*)w, (__bf16*)da, ldd, ldw, ldda, 0, M, K, N, 0, 0, 1, N, 1};
   TilePair kind = linear_gradient_tiles(M, K, N, parts);
