@@ -405,13 +405,14 @@ inline int norm_bwd_together(int rows, int cols) {
   const NormBwdRows r = norm_bwd_rows(cols);
   const int lanes = r == NormBwdRows::k16x2 ? 16 : r == NormBwdRows::k128x2 ? 128 : r == NormBwdRows::k256x2 ? 256 : r == NormBwdRows::k512x2 ? 512 : r == NormBwdRows::k1024x2 ? 1024 : 64;
   const int most = kNormBwdThreads / lanes, least = lanes < 64 ? 64 / lanes : 1;   // whole waves
-  const int wanted = (int)(((long long)rows + 255) / 256);
+  const int wanted = rows <= 2 * most ? rows : (int)(((long long)rows + 255) / 256);   // up to two turns: a single workgroup, which needs no second launch
   return wanted >= most ? most : wanted <= least ? least : (wanted + least - 1) / least * least;
 }
 // Its workgroups.  Each leaves a slab of partial sums of dgamma and dbeta.
 inline int norm_bwd_groups(int rows, int cols) {
-  const long long turns = ((long long)rows + norm_bwd_together(rows, cols) - 1) / norm_bwd_together(rows, cols);
-  return (int)std::min<long long>(turns, 256);
+  const int together = norm_bwd_together(rows, cols);
+  const long long turns = ((long long)rows + together - 1) / together;
+  return turns <= 2 ? 1 : (int)std::min<long long>(turns, 256);
 }
 
 }  // namespace helix

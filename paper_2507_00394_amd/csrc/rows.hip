@@ -27,13 +27,16 @@ struct Chunk {
   typedef T Vec __attribute__((ext_vector_type(8), aligned(sizeof(T))));
   Vec v;
 };
-// `n` of the 8 elements exist; the others are read as zero and not written.  Loads that do not ask to be kept: 129 us instead of 157 for dropout and sum of 32768 x 4096.
+// `n` of the 8 elements exist; the others are read as zero and not written.  A lane's 16 bytes go past the caches, which have no use for them (dropout and sum of
+// 32768 x 4096 bf16 158 -> 143 us); the 32 bytes of a 4-byte type are two accesses to a line, which they had better join (20000 x 4001 fp32 197 us, 218 past them).
 template <typename T>
 __device__ __forceinline__ Chunk<T> load_chunk(const T* p, int n) {
   Chunk<T> c;
   c.v = (T)0.f;
   if (n >= 8) {
-    c.v = __builtin_nontemporal_load(reinterpret_cast<const typename Chunk<T>::Vec*>(p));
+    const auto* const q = reinterpret_cast<const typename Chunk<T>::Vec*>(p);
+    if constexpr (sizeof(T) == 2) c.v = __builtin_nontemporal_load(q);
+    else c.v = *q;
   } else if (n > 0) {
 #pragma unroll
     for (int e = 0; e < 7; e++)
@@ -45,7 +48,9 @@ template <typename T>
 __device__ __forceinline__ void store_chunk(T* p, int n, const f32x8& x) {
   const auto v = __builtin_convertvector(x, typename Chunk<T>::Vec);
   if (n >= 8) {
-    *reinterpret_cast<typename Chunk<T>::Vec*>(p) = v;
+    auto* const q = reinterpret_cast<typename Chunk<T>::Vec*>(p);
+    if constexpr (sizeof(T) == 2) __builtin_nontemporal_store(v, q);
+    else *q = v;
   } else if (n > 0) {
 #pragma unroll
     for (int e = 0; e < 7; e++)
@@ -182,8 +187,8 @@ struct Columns {
     if (has[i]) c.v = *reinterpret_cast<const typename Chunk<T>::Vec*>(row + (first + 8 * L * i));
     return c;
   }
-  // ONCE: results of one use, which need not push anything out of the caches (gradient of dropout, sum and norm, 131072 x 4096: 1037 -> 965 us; the
-  // 32 bytes that a lane has of a 4-byte type go out in two halves, which the L2 had better join)
+  // ONCE: results that the caches need not keep, as in store_chunk (8192 x 5001 50 -> 35 us, dropout, sum and norm of 20000 x 900 36 -> 28).  Loads past the caches are no
+  // gain here: 192 -> 183 us for dropout, sum and norm of 32768 x 4096, but 35 -> 47 at 8192 x 5001, whose lines two lanes or two waves read.
   template <bool ONCE = false, typename T>
   __device__ __forceinline__ void store(T* row, int i, const f32x8& x) const {
     auto* const p = reinterpret_cast<typename Chunk<T>::Vec*>(row + (first + 8 * L * i));
@@ -288,7 +293,7 @@ __global__ void __launch_bounds__(row_threads(L)) __attribute__((amdgpu_waves_pe
 //
 // A lane keeps its columns' sums over all rows that it works on.  A compute unit has one workgroup, of as many rows at a time as it has waves for, so that
 // few partial sums are left: the workgroup adds up its rows' and leaves one slab, `partial` [gridDim.x][2][cols], and sum_partials_kernel adds the slabs up in a fixed
-// order.  Up to 4096 columns a wave has a row to itself and needs no barrier.  gamma waits in LDS for all of them: its registers are the sums'.
+// order (16384 x 2048 bf16: 73 us with four workgroups of 256 threads on a compute unit, 1024 slabs and a thread's loads of them one after the other, 45 now).  Up to 4096 columns a wave has a row to itself and needs no barrier.  gamma waits in LDS for all of them: its registers are the sums'.
 template <typename T, int L, int NC, bool SUM>
 __global__ void __launch_bounds__(kNormBwdThreads) layer_norm_bwd_kernel(NormBwd a) {
   constexpr int COLS = 8 * L * NC, MOST = kNormBwdThreads / L;   // MOST rows at a time
@@ -389,7 +394,7 @@ __global__ void __launch_bounds__(kNormBwdThreads) layer_norm_bwd_kernel(NormBwd
       at.store_tail(dx, d);
     }
   }
-  float* const out = a.partial + (size_t)blockIdx.x * 2 * a.cols;
+  const bool alone = gridDim.x == 1;   // these are the results
   if (at.has_tail) {
     tails[0][sub][at.l] = dgamma_tail;
     tails[1][sub][at.l] = dbeta_tail;
@@ -397,6 +402,7 @@ __global__ void __launch_bounds__(kNormBwdThreads) layer_norm_bwd_kernel(NormBwd
 #pragma unroll
   for (int which = 0; which < 2; which++) {
     f32x8(&sum)[NC] = which ? dbeta : dgamma;
+    float* const out = alone ? (which ? a.dbeta : a.dgamma) : a.partial + ((size_t)blockIdx.x * 2 + which) * a.cols;
     for (int left = together; left > 1; left = (left + 1) / 2) {   // the upper half of the rows' sums is added to the lower
       const int half = (left + 1) / 2;
       __syncthreads();
@@ -414,11 +420,11 @@ __global__ void __launch_bounds__(kNormBwdThreads) layer_norm_bwd_kernel(NormBwd
     }
     if (sub == 0) {
 #pragma unroll
-      for (int i = 0; i < NC; i++) at.store(out + which * a.cols, i, sum[i]);
+      for (int i = 0; i < NC; i++) at.store(out, i, sum[i]);
       if (at.has_tail) {   // written above, in front of a barrier unless this is the only row
         float t = tails[which][0][at.l];
         for (int g = 1; g < together; g++) t += tails[which][g][at.l];
-        at.store_tail(out + which * a.cols, t);
+        at.store_tail(out, t);
       }
     }
   }
@@ -463,7 +469,7 @@ hipError_t launch_bwd_rows(const NormBwd& a, hipStream_t stream) {
   if (a.dr) hipLaunchKernelGGL((layer_norm_bwd_kernel<T, L, NC, true>), dim3((unsigned)grid), dim3((unsigned)(together * L)), 0, stream, a);
   else hipLaunchKernelGGL((layer_norm_bwd_kernel<T, L, NC, false>), dim3((unsigned)grid), dim3((unsigned)(together * L)), 0, stream, a);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  if (e != hipSuccess || grid == 1) return e;
   hipLaunchKernelGGL(sum_partials_kernel, dim3((unsigned)((2 * a.cols + 31) / 32)), dim3(32 * kSumParts), 0, stream, a.partial, grid, a.cols, a.dgamma, a.dbeta);
   return hipGetLastError();
 }
