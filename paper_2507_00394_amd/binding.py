@@ -349,11 +349,13 @@ def _refuse(name, t, device, what):
     raise ValueError(f"{name}: need {what}")
 
 
-def _rows(name, t):
-    """(shape, element type) of an activation."""
-    if t.dim() != 2 or t.dtype not in _TYPES:
+def _first(name, t, stream):
+    """(device, shape, element type, pointer, elements between rows) of a call's first activation, which the others have to be like."""
+    dev = _current(t, stream)
+    shape, dtype = t.shape, t.dtype
+    if len(shape) != 2 or dtype not in _TYPES:
         raise ValueError(f"{name}: need a matrix of bfloat16, float16 or float32")
-    return t.shape, t.dtype
+    return dev, shape, dtype, *_activation(name, t, shape, dtype, dev)
 
 
 def _activation(name, t, shape, dtype, device):
@@ -391,9 +393,7 @@ def _workspace(workspace, device):
 def helix_dropout_add_fwd(x, residual, out, p, rng, first_row=0, stream=None):
     """out[M,E] <- residual + dropout(x); residual None: dropout(x).  rng: CUDA int64 tensor [seed, offset] (None where p == 0);
     row i takes the random numbers of row first_row + i."""
-    dev = _current(x, stream)
-    shape, dtype = _rows("x", x)
-    px, ldx = _activation("x", x, shape, dtype, dev)
+    dev, shape, dtype, px, ldx = _first("x", x, stream)
     pr, ldr = (None, 0) if residual is None else _activation("residual", residual, shape, dtype, dev)
     po, ldo = _activation("out", out, shape, dtype, dev)
     _raise(lib().helix_dropout_add_fwd(px, ldx, pr, ldr, po, ldo, shape[0], shape[1], _TYPES[dtype], float(p), _generator(rng, dev), int(first_row), _stream(stream)),
@@ -402,9 +402,7 @@ def helix_dropout_add_fwd(x, residual, out, p, rng, first_row=0, stream=None):
 
 def helix_dropout_add_bwd(dout, dx, p, rng, first_row=0, stream=None):
     """dx[M,E] <- gradient of the dropped-out branch; the residual's gradient is dout itself."""
-    dev = _current(dout, stream)
-    shape, dtype = _rows("dout", dout)
-    pg, ldg = _activation("dout", dout, shape, dtype, dev)
+    dev, shape, dtype, pg, ldg = _first("dout", dout, stream)
     px, ldx = _activation("dx", dx, shape, dtype, dev)
     _raise(lib().helix_dropout_add_bwd(pg, ldg, px, ldx, shape[0], shape[1], _TYPES[dtype], float(p), _generator(rng, dev), int(first_row), _stream(stream)),
            "helix_dropout_add_bwd")
@@ -412,10 +410,8 @@ def helix_dropout_add_bwd(dout, dx, p, rng, first_row=0, stream=None):
 
 def helix_layer_norm_fwd(x, gamma, beta, y, mean, rstd, eps=1e-5, stream=None):
     """y[M,E], mean[M], rstd[M] <- layer norm of the rows of x; gamma, beta: fp32 [E].  mean and rstd may be None."""
-    dev = _current(x, stream)
-    shape, dtype = _rows("x", x)
+    dev, shape, dtype, px, ldx = _first("x", x, stream)
     M, E = shape
-    px, ldx = _activation("x", x, shape, dtype, dev)
     py, ldy = _activation("y", y, shape, dtype, dev)
     _raise(lib().helix_layer_norm_fwd(px, ldx, _vector("gamma", gamma, E, dev), _vector("beta", beta, E, dev), py, ldy,
                                       None if mean is None else _vector("mean", mean, M, dev), None if rstd is None else _vector("rstd", rstd, M, dev),
@@ -429,11 +425,9 @@ def helix_layer_norm_bwd_workspace_bytes(M, E) -> int:
 def helix_layer_norm_bwd(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, workspace, stream=None):
     """dx[M,E], dgamma[E], dbeta[E] <- gradients of helix_layer_norm_fwd; workspace: uint8 CUDA tensor of
     helix_layer_norm_bwd_workspace_bytes(M, E) bytes."""
-    dev = _current(x, stream)
-    shape, dtype = _rows("x", x)
+    dev, shape, dtype, px, ldx = _first("x", x, stream)
     M, E = shape
     pdy, lddy = _activation("dy", dy, shape, dtype, dev)
-    px, ldx = _activation("x", x, shape, dtype, dev)
     pdx, lddx = _activation("dx", dx, shape, dtype, dev)
     pw, nw = _workspace(workspace, dev)
     _raise(lib().helix_layer_norm_bwd(pdy, lddy, px, ldx, _vector("gamma", gamma, E, dev), _vector("mean", mean, M, dev), _vector("rstd", rstd, M, dev), pdx, lddx,
@@ -443,10 +437,8 @@ def helix_layer_norm_bwd(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, workspace,
 
 def helix_dropout_add_layer_norm_fwd(x, residual, s, gamma, beta, y, mean, rstd, p, rng, eps=1e-5, first_row=0, stream=None):
     """s <- residual + dropout(x), y, mean, rstd <- layer norm of s (see helix_dropout_add_fwd and helix_layer_norm_fwd)."""
-    dev = _current(x, stream)
-    shape, dtype = _rows("x", x)
+    dev, shape, dtype, px, ldx = _first("x", x, stream)
     M, E = shape
-    px, ldx = _activation("x", x, shape, dtype, dev)
     pr, ldr = _activation("residual", residual, shape, dtype, dev)
     ps, lds = _activation("s", s, shape, dtype, dev)
     py, ldy = _activation("y", y, shape, dtype, dev)
@@ -457,12 +449,10 @@ def helix_dropout_add_layer_norm_fwd(x, residual, s, gamma, beta, y, mean, rstd,
 
 def helix_dropout_add_layer_norm_bwd(dy, ds, s, gamma, mean, rstd, dx, dresidual, dgamma, dbeta, workspace, p, rng, first_row=0, stream=None):
     """dresidual <- ds + gradient of the layer norm of s, dx <- its dropped-out share, dgamma, dbeta.  ds may be None."""
-    dev = _current(s, stream)
-    shape, dtype = _rows("s", s)
+    dev, shape, dtype, ps, lds = _first("s", s, stream)
     M, E = shape
     pdy, lddy = _activation("dy", dy, shape, dtype, dev)
     pds, ldds = (None, 0) if ds is None else _activation("ds", ds, shape, dtype, dev)
-    ps, lds = _activation("s", s, shape, dtype, dev)
     pdx, lddx = _activation("dx", dx, shape, dtype, dev)
     pdr, lddr = _activation("dresidual", dresidual, shape, dtype, dev)
     pw, nw = _workspace(workspace, dev)

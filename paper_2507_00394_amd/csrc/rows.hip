@@ -297,7 +297,7 @@ __global__ void __launch_bounds__(row_threads(L)) __attribute__((amdgpu_waves_pe
 template <typename T, int L, int NC, bool SUM>
 __global__ void __launch_bounds__(kNormBwdThreads) layer_norm_bwd_kernel(NormBwd a) {
   constexpr int COLS = 8 * L * NC, MOST = kNormBwdThreads / L;   // MOST rows at a time
-  __shared__ __align__(16) float lds[(MOST > 2 ? MOST / 2 : 1) * COLS];
+  __shared__ __align__(16) float lds[(MOST > 1 ? 2 * (MOST / 2) : 1) * COLS];   // gamma; at the end the sums of half of the rows
   __shared__ float red[2][kNormBwdThreads / 64][2], tails[2][MOST][8];
   const int sub = row_of_lane<L>(), together = blockDim.x / L;
   const Columns<L, NC> at(a.cols);
@@ -399,33 +399,32 @@ __global__ void __launch_bounds__(kNormBwdThreads) layer_norm_bwd_kernel(NormBwd
     tails[0][sub][at.l] = dgamma_tail;
     tails[1][sub][at.l] = dbeta_tail;
   }
+  for (int left = together; left > 1; left = (left + 1) / 2) {   // the upper half of the rows' sums is added to the lower
+    const int half = (left + 1) / 2;
+    __syncthreads();
+    f32x4* const mine = reinterpret_cast<f32x4*>(lds) + (size_t)(sub >= half ? sub - half : sub) * (COLS / 2) + at.l;
+    if (sub >= half && sub < left)
+#pragma unroll
+      for (int i = 0; i < 2 * NC; i++) {
+        const f32x8& sum = i < NC ? dgamma[i % NC] : dbeta[i % NC];
+        mine[2 * i * L] = __builtin_shufflevector(sum, sum, 0, 1, 2, 3);
+        mine[(2 * i + 1) * L] = __builtin_shufflevector(sum, sum, 4, 5, 6, 7);
+      }
+    __syncthreads();
+    if (sub + half < left)
+#pragma unroll
+      for (int i = 0; i < 2 * NC; i++) (i < NC ? dgamma[i % NC] : dbeta[i % NC]) += __builtin_shufflevector(mine[2 * i * L], mine[(2 * i + 1) * L], 0, 1, 2, 3, 4, 5, 6, 7);
+  }
+  if (sub != 0) return;
 #pragma unroll
   for (int which = 0; which < 2; which++) {
-    f32x8(&sum)[NC] = which ? dbeta : dgamma;
     float* const out = alone ? (which ? a.dbeta : a.dgamma) : a.partial + ((size_t)blockIdx.x * 2 + which) * a.cols;
-    for (int left = together; left > 1; left = (left + 1) / 2) {   // the upper half of the rows' sums is added to the lower
-      const int half = (left + 1) / 2;
-      __syncthreads();
-      f32x4* const mine = reinterpret_cast<f32x4*>(lds) + (size_t)(sub >= half ? sub - half : sub) * (COLS / 4) + at.l;
-      if (sub >= half && sub < left)
 #pragma unroll
-        for (int i = 0; i < NC; i++) {
-          mine[2 * i * L] = __builtin_shufflevector(sum[i], sum[i], 0, 1, 2, 3);
-          mine[(2 * i + 1) * L] = __builtin_shufflevector(sum[i], sum[i], 4, 5, 6, 7);
-        }
-      __syncthreads();
-      if (sub + half < left)
-#pragma unroll
-        for (int i = 0; i < NC; i++) sum[i] += __builtin_shufflevector(mine[2 * i * L], mine[(2 * i + 1) * L], 0, 1, 2, 3, 4, 5, 6, 7);
-    }
-    if (sub == 0) {
-#pragma unroll
-      for (int i = 0; i < NC; i++) at.store(out, i, sum[i]);
-      if (at.has_tail) {   // written above, in front of a barrier unless this is the only row
-        float t = tails[which][0][at.l];
-        for (int g = 1; g < together; g++) t += tails[which][g][at.l];
-        at.store_tail(out, t);
-      }
+    for (int i = 0; i < NC; i++) at.store(out, i, which ? dbeta[i] : dgamma[i]);
+    if (at.has_tail) {   // written above, in front of a barrier unless this is the only row
+      float t = tails[which][0][at.l];
+      for (int g = 1; g < together; g++) t += tails[which][g][at.l];
+      at.store_tail(out, t);
     }
   }
 }
