@@ -365,7 +365,7 @@ def _activation(name, t, shape, dtype, device):
     ld, one = t.stride()
     if one != 1 and shape[1] > 1:
         raise ValueError(f"{name}: need contiguous rows")
-    return t.data_ptr(), ld if shape[0] > 1 else max(ld, shape[1])   # a single row has no next one
+    return t.data_ptr(), ld if shape[0] > 1 else shape[1]   # a single row has no next one
 
 
 def _vector(name, t, n, device):

@@ -209,3 +209,21 @@ def test_the_framework_runs_it_as_the_linear_layer_does():
     hx.helix_gated_linear_fwd(a, w, h, gu=gu)
     hx.helix_qkv_linear_fwd(a, w, same)
     _within("gu", gu, _f64(same), 2 * HALF * np.abs(_f64(same)) + 2 * _off_gu(_f64(a), _f64(w)))
+
+
+def test_the_pitch_of_a_single_row_counts_for_nothing():
+    """One token taken from a buffer whose rows are an odd number of elements apart: there is no next row."""
+    from paper_2507_00394_amd import binding as hx
+
+    K, F = 256, 192
+    w = _draw(1, (K, 2 * F), K ** -0.5)
+    row = lambda n: torch.as_strided(torch.zeros(n, dtype=torch.bfloat16, device="cuda"), (1, n), (n + 3, 1))
+    results = []
+    for new in (row, lambda n: torch.zeros(1, n, dtype=torch.bfloat16, device="cuda")):
+        a, dh, h, gu, da, dw = new(K), new(F), new(F), new(2 * F), new(K), torch.empty_like(w)
+        a.copy_(_draw(2, (1, K)))
+        dh.copy_(_draw(3, (1, F)))
+        hx.helix_gated_linear_fwd(a, w, h, gu=gu)
+        hx.helix_gated_linear_bwd(a, w, dh, da, dw, torch.empty(hx.helix_gated_linear_bwd_workspace_bytes(1, K, F), dtype=torch.uint8, device="cuda"), gu=gu)
+        results.append((h, gu, da, dw))
+    assert all(torch.equal(x, y) and y.abs().max() > 0 for x, y in zip(*results))
