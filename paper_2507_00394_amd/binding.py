@@ -349,6 +349,17 @@ def _refuse(name, t, device, what):
     raise ValueError(f"{name}: need {what}")
 
 
+def _length(n):
+    """A length for the library, whose lengths have 32 bits: one that has more is 0 there, a bad shape, and not what is left of it."""
+    return n if -0x80000000 <= n <= 0x7fffffff else 0
+
+
+def _row(n):
+    """A first_row for the library, in 64 bits: what has more is -1 there, a bad shape."""
+    n = int(n)
+    return n if 0 <= n < 1 << 63 else -1
+
+
 def _first(name, t, stream):
     """(device, shape, element type, pointer, elements between rows) of a call's first activation, which the others have to be like."""
     dev = _current(t, stream)
@@ -396,7 +407,7 @@ def helix_dropout_add_fwd(x, residual, out, p, rng, first_row=0, stream=None):
     dev, shape, dtype, px, ldx = _first("x", x, stream)
     pr, ldr = (None, 0) if residual is None else _activation("residual", residual, shape, dtype, dev)
     po, ldo = _activation("out", out, shape, dtype, dev)
-    _raise(lib().helix_dropout_add_fwd(px, ldx, pr, ldr, po, ldo, shape[0], shape[1], _TYPES[dtype], float(p), _generator(rng, dev), int(first_row), _stream(stream)),
+    _raise(lib().helix_dropout_add_fwd(px, ldx, pr, ldr, po, ldo, _length(shape[0]), _length(shape[1]), _TYPES[dtype], float(p), _generator(rng, dev), _row(first_row), _stream(stream)),
            "helix_dropout_add_fwd")
 
 
@@ -404,7 +415,7 @@ def helix_dropout_add_bwd(dout, dx, p, rng, first_row=0, stream=None):
     """dx[M,E] <- gradient of the dropped-out branch; the residual's gradient is dout itself."""
     dev, shape, dtype, pg, ldg = _first("dout", dout, stream)
     px, ldx = _activation("dx", dx, shape, dtype, dev)
-    _raise(lib().helix_dropout_add_bwd(pg, ldg, px, ldx, shape[0], shape[1], _TYPES[dtype], float(p), _generator(rng, dev), int(first_row), _stream(stream)),
+    _raise(lib().helix_dropout_add_bwd(pg, ldg, px, ldx, _length(shape[0]), _length(shape[1]), _TYPES[dtype], float(p), _generator(rng, dev), _row(first_row), _stream(stream)),
            "helix_dropout_add_bwd")
 
 
@@ -415,11 +426,11 @@ def helix_layer_norm_fwd(x, gamma, beta, y, mean, rstd, eps=1e-5, stream=None):
     py, ldy = _activation("y", y, shape, dtype, dev)
     _raise(lib().helix_layer_norm_fwd(px, ldx, _vector("gamma", gamma, E, dev), _vector("beta", beta, E, dev), py, ldy,
                                       None if mean is None else _vector("mean", mean, M, dev), None if rstd is None else _vector("rstd", rstd, M, dev),
-                                      M, E, _TYPES[dtype], float(eps), _stream(stream)), "helix_layer_norm_fwd")
+                                      _length(M), _length(E), _TYPES[dtype], float(eps), _stream(stream)), "helix_layer_norm_fwd")
 
 
 def helix_layer_norm_bwd_workspace_bytes(M, E) -> int:
-    return int(lib().helix_layer_norm_bwd_workspace_bytes(M, E))
+    return int(lib().helix_layer_norm_bwd_workspace_bytes(_length(M), _length(E)))
 
 
 def helix_layer_norm_bwd(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, workspace, stream=None):
@@ -431,7 +442,7 @@ def helix_layer_norm_bwd(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, workspace,
     pdx, lddx = _activation("dx", dx, shape, dtype, dev)
     pw, nw = _workspace(workspace, dev)
     _raise(lib().helix_layer_norm_bwd(pdy, lddy, px, ldx, _vector("gamma", gamma, E, dev), _vector("mean", mean, M, dev), _vector("rstd", rstd, M, dev), pdx, lddx,
-                                      _vector("dgamma", dgamma, E, dev), _vector("dbeta", dbeta, E, dev), pw, nw, M, E, _TYPES[dtype], _stream(stream)),
+                                      _vector("dgamma", dgamma, E, dev), _vector("dbeta", dbeta, E, dev), pw, nw, _length(M), _length(E), _TYPES[dtype], _stream(stream)),
            "helix_layer_norm_bwd")
 
 
@@ -444,7 +455,7 @@ def helix_dropout_add_layer_norm_fwd(x, residual, s, gamma, beta, y, mean, rstd,
     py, ldy = _activation("y", y, shape, dtype, dev)
     _raise(lib().helix_dropout_add_layer_norm_fwd(px, ldx, pr, ldr, ps, lds, _vector("gamma", gamma, E, dev), _vector("beta", beta, E, dev), py, ldy,
                                                   None if mean is None else _vector("mean", mean, M, dev), None if rstd is None else _vector("rstd", rstd, M, dev),
-                                                  M, E, _TYPES[dtype], float(p), _generator(rng, dev), int(first_row), float(eps), _stream(stream)), "helix_dropout_add_layer_norm_fwd")
+                                                  _length(M), _length(E), _TYPES[dtype], float(p), _generator(rng, dev), _row(first_row), float(eps), _stream(stream)), "helix_dropout_add_layer_norm_fwd")
 
 
 def helix_dropout_add_layer_norm_bwd(dy, ds, s, gamma, mean, rstd, dx, dresidual, dgamma, dbeta, workspace, p, rng, first_row=0, stream=None):
@@ -458,7 +469,7 @@ def helix_dropout_add_layer_norm_bwd(dy, ds, s, gamma, mean, rstd, dx, dresidual
     pw, nw = _workspace(workspace, dev)
     _raise(lib().helix_dropout_add_layer_norm_bwd(pdy, lddy, pds, ldds, ps, lds, _vector("gamma", gamma, E, dev), _vector("mean", mean, M, dev),
                                                   _vector("rstd", rstd, M, dev), pdx, lddx, pdr, lddr, _vector("dgamma", dgamma, E, dev),
-                                                  _vector("dbeta", dbeta, E, dev), pw, nw, M, E, _TYPES[dtype], float(p), _generator(rng, dev), int(first_row),
+                                                  _vector("dbeta", dbeta, E, dev), pw, nw, _length(M), _length(E), _TYPES[dtype], float(p), _generator(rng, dev), _row(first_row),
                                                   _stream(stream)), "helix_dropout_add_layer_norm_bwd")
 
 
@@ -483,11 +494,11 @@ def helix_gated_linear_fwd(a, w, h, gu=None, activation="silu", stream=None):
     pw, ldw = _activation("w", w, (K, 2 * F), _BF16, dev)
     pg, ldg = (None, 0) if gu is None else _activation("gu", gu, (M, 2 * F), _BF16, dev)
     ph, ldh = _activation("h", h, (M, F), _BF16, dev)
-    _raise(lib().helix_gated_linear_fwd(pa, lda, pw, ldw, pg, ldg, ph, ldh, M, K, F, act, _stream(stream)), "helix_gated_linear_fwd")
+    _raise(lib().helix_gated_linear_fwd(pa, lda, pw, ldw, pg, ldg, ph, ldh, _length(M), _length(K), _length(F), act, _stream(stream)), "helix_gated_linear_fwd")
 
 
 def helix_gated_linear_bwd_workspace_bytes(M, K, F) -> int:
-    return int(lib().helix_gated_linear_bwd_workspace_bytes(M, K, F))
+    return int(lib().helix_gated_linear_bwd_workspace_bytes(_length(M), _length(K), _length(F)))
 
 
 def helix_gated_linear_bwd(a, w, dh, da, dw, workspace, gu=None, activation="silu", stream=None):
@@ -502,4 +513,4 @@ def helix_gated_linear_bwd(a, w, dh, da, dw, workspace, gu=None, activation="sil
     pda, ldda = _activation("da", da, (M, K), _BF16, dev)
     pdw, lddw = _activation("dw", dw, (K, 2 * F), _BF16, dev)
     pws, nws = _workspace(workspace, dev)
-    _raise(lib().helix_gated_linear_bwd(pa, lda, pw, ldw, pg, ldg, ph, ldh, pda, ldda, pdw, lddw, pws, nws, M, K, F, act, _stream(stream)), "helix_gated_linear_bwd")
+    _raise(lib().helix_gated_linear_bwd(pa, lda, pw, ldw, pg, ldg, ph, ldh, pda, ldda, pdw, lddw, pws, nws, _length(M), _length(K), _length(F), act, _stream(stream)), "helix_gated_linear_bwd")

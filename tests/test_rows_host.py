@@ -91,3 +91,26 @@ def test_binding_refuses(L):
         hx.helix_dropout_add_fwd(x, None, x, 0.1, torch.zeros(2, dtype=torch.int64))
     with pytest.raises(ValueError):
         hx.helix_dropout_add_bwd(x.double(), x, 0.1, None)
+
+
+def test_lengths_of_more_than_32_bits_are_refused(L, monkeypatch):
+    """The library's lengths have 32 bits: what is longer must not arrive there as what is left of it."""
+    long = 2 ** 32 + 3
+    assert hx.helix_layer_norm_bwd_workspace_bytes(long, 64) == 0 and hx.helix_layer_norm_bwd_workspace_bytes(4, 2 ** 32 + 64) == 0
+    for shape in ((2 ** 32 + 4, 256, 128), (4, 2 ** 32 + 256, 128), (4, 256, 2 ** 32 + 128)):
+        assert hx.helix_gated_linear_bwd_workspace_bytes(*shape) == 0
+    monkeypatch.setattr(hx, "_current", lambda t, stream: -1)     # host memory stands for the device's: nothing gets as far as a kernel
+    monkeypatch.setattr(hx, "_stream", lambda stream: None)
+    for M, E in ((long, 1), (1, long)):
+        x = torch.empty_strided((M, E), (1, 1) if E == 1 else (E, 1), dtype=torch.float16)   # never touched, so it takes no memory
+        with pytest.raises(hx.HelixStatusError) as e:
+            hx.helix_dropout_add_fwd(x, None, x, 0.0, None)
+        assert e.value.status == 2
+        with pytest.raises(hx.HelixStatusError) as e:
+            hx.helix_dropout_add_bwd(x, x, 0.0, None)
+        assert e.value.status == 2
+    x, rng = torch.zeros(4, 64), torch.zeros(2, dtype=torch.int64)
+    for first in (-1, 2 ** 32, 2 ** 64, 2 ** 64 - 1, -2 ** 64):
+        with pytest.raises(hx.HelixStatusError) as e:
+            hx.helix_dropout_add_fwd(x, None, x, 0.5, rng, first_row=first)
+        assert e.value.status == 2
