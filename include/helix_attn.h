@@ -240,6 +240,8 @@ size_t helix_qkv_linear_bwd_workspace_bytes(int M, int K, int N);
  * No alignment is asked for beyond that of an element; rows that start on 16-byte boundaries are the
  * fastest.  Parameters, their gradients and the row statistics are contiguous fp32.  Arithmetic is fp32;
  * activations are rounded once, when they are stored.  Padding between the rows is not written.
+ * An output activation may take the place of an input activation of its call (the same pointer and ld*: the residual
+ * stream updated in place); every other overlap is excluded, as everywhere.
  *
  * Dropout with probability p, 0 <= p < 1 (HELIX_ERR_BAD_PROBABILITY): an element is dropped with the
  * probability p' = cut / 2^16, cut = round(p * 2^16) (at most 2^16 - 1), and multiplied by 1 / (1 - p') otherwise.
@@ -305,7 +307,8 @@ int helix_dropout_add_layer_norm_bwd(const void* dy, long long lddy, const void*
  * ld* as for helix_qkv_linear_fwd: 16-byte aligned, ld* at least the row length, a multiple of 8, at most 2^22 (HELIX_ERR_BAD_STRIDE).
  * The down projection h -> [M][K] is helix_qkv_linear_fwd / _bwd with F, then a multiple of 128, in the place of K.
  * workspace: device memory of at least helix_gated_linear_bwd_workspace_bytes(M, K, F) bytes, 256-byte aligned, contents undefined
- * afterwards: [dg du], and what helix_qkv_linear_bwd keeps there.  No atomics: every bit is reproduced. */
+ * afterwards: [dg du], and what helix_qkv_linear_bwd keeps there.  No atomics: every bit is reproduced.  M, K and F decide which
+ * tiles a call takes and with them the order of its sums: a token's results in calls of different M agree within rounding. */
 int helix_gated_linear_fwd(const void* a, long long lda, const void* w, long long ldw, void* gu, long long ldgu,
                            void* h, long long ldh, int M, int K, int F, int activation, void* stream);
 int helix_gated_linear_bwd(const void* a, long long lda, const void* w, long long ldw, const void* gu, long long ldgu,

@@ -361,6 +361,44 @@ def test_graph_replays_draw_new_numbers_when_the_offset_moves():
             assert n == 8 or torch.equal(a, b), f"output {n} of the replay with offset {step}"
 
 
+@pytest.mark.parametrize("kind", TYPES)
+@pytest.mark.parametrize("M,E", [(3, 7), (40, 520), (21, 1025), (9, 4096), (300, 5001), (3, 16384)])
+def test_in_place(kind, M, E):
+    """An output in the place of any input of its call (pointer and pitch) has the bits that it has elsewhere."""
+    from paper_2507_00394_amd import binding as hx
+
+    dtype, rng = TYPES[kind], _rng()
+    gamma, beta = _params(E)
+    src = [_draw(n, M, E, dtype) for n in range(4)]
+    new = lambda: [torch.nn.functional.pad(t, (0, 5))[:, :E] for t in src]
+    stat = lambda: (torch.empty(M, device="cuda"), torch.empty(M, device="cuda"))
+    mean, rstd = stat()
+    hx.helix_layer_norm_fwd(src[1], gamma, beta, torch.empty_like(src[1]), mean, rstd)
+    ws, grads = _bwd_buffers(M, E, dtype)
+
+    def compare(call, outputs, places):
+        """call(inputs, outputs); outputs: how many; places: (output, input whose place it takes)."""
+        want = [torch.empty_like(src[0]) for _ in range(outputs)]
+        more = call(new(), want)
+        want += [t.clone() for t in more]
+        for place in places:
+            ins, outs = new(), [torch.empty_like(src[0]) for _ in range(outputs)]
+            for o, i in place:
+                outs[o] = ins[i]
+            more = call(ins, outs)
+            assert all(torch.equal(a, b) for a, b in zip(want, [*outs, *more])), place
+
+    compare(lambda i, o: hx.helix_dropout_add_fwd(i[0], i[1], o[0], 0.3, rng) or [], 1, [[(0, 0)], [(0, 1)]])
+    compare(lambda i, o: hx.helix_dropout_add_bwd(i[0], o[0], 0.3, rng) or [], 1, [[(0, 0)]])
+    st = stat()
+    compare(lambda i, o: hx.helix_layer_norm_fwd(i[0], gamma, beta, o[0], *st) or st, 1, [[(0, 0)]])
+    compare(lambda i, o: hx.helix_layer_norm_bwd(i[0], i[1], gamma, mean, rstd, o[0], *grads, ws) or grads, 1, [[(0, 0)], [(0, 1)]])
+    compare(lambda i, o: hx.helix_dropout_add_layer_norm_fwd(i[0], i[1], o[0], gamma, beta, o[1], *st, 0.3, rng) or st, 2,
+            [[(0, 1)], [(0, 0)], [(1, 0)], [(1, 1)], [(0, 1), (1, 0)], [(0, 0), (1, 1)]])
+    compare(lambda i, o: hx.helix_dropout_add_layer_norm_bwd(i[0], i[2], i[1], gamma, mean, rstd, o[0], o[1], *grads, ws, 0.3, rng) or grads, 2,
+            [[(0, 0)], [(0, 1)], [(0, 2)], [(1, 0)], [(1, 1)], [(1, 2)], [(0, 0), (1, 2)], [(0, 2), (1, 0)], [(0, 1), (1, 2)]])
+
+
 def test_another_stream():
     M, E = 2000, 1030
     x, r, g, (gamma, beta) = _draw(1, M, E, torch.bfloat16), _draw(2, M, E, torch.bfloat16), _draw(3, M, E, torch.bfloat16), _params(E)
