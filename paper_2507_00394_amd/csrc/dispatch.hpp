@@ -355,8 +355,11 @@ inline int split_weight_parts(int M, int K, int N) {
   return std::min(linear_bwd_weight_parts(M, K, N), (128 + tiles - 1) / tiles);
 }
 
-// The gated projections of few rows (skinny.hip; on tiles / so, us: 1 x 2048 x 5504 12.5 / 11.5, 8 x 5120 x 1728 25.9 / 18.9, 32 x 1024 x 8192 9.6 / 9.4, 1 x 4096 x 11008 36.2 / 37.5).
+// The gated projections of few rows (skinny.hip): up to 32, and where all of its workgroups, 32 columns each, run at once; behind that the tiles fetch as fast.  On tiles / so, us,
+// M x K x F: 1 x 2048 x 5504 12.5 / 10.2, 8 x 1024 x 2752 7.9 / 6.0, 16 x 4096 x 1408 21.3 / 17.0, 16 x 512 x 640 5.0 / 3.9, 17 x 1024 x 2752 7.9 / 6.9, 32 x 2048 x 5504 12.7 / 12.6,
+// 32 x 1024 x 8192 9.4 / 9.3, 32 x 4096 x 8192 41.3 / 42.8; 16 x 2048 x 11008 21.1 / 34.5, 32 x 4096 x 11008 41.8 / 71.8.
 inline bool gated_skinny(int M) { return M <= 32; }
+inline bool gated_few(int M, int F) { return gated_skinny(M) && F <= 32 * 256; }
 // The gated projections' tiles: 256 x 128, 128 x 64 and 64 x 64 elements of h, twice as many columns of the product.  Time models as those of linear_tile, fitted to 97 shapes (33 to
 // 30000 tokens, K to 5120, F to 11008): us per 1000 contraction indices with the chip full and alone, for the start and end of a round and of the last one, per MB of h, per MB
 // read (the weights by every XCD).

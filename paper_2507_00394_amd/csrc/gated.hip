@@ -225,7 +225,7 @@ hipError_t launch_tiles(const Gated& p, hipStream_t stream) {
 }
 template <bool GRAD, Activation ACT>
 hipError_t launch_projections(const Gated& p, hipStream_t stream) {
-  if (gated_skinny(p.M)) return launch_skinny_projections(p, GRAD, ACT, stream);
+  if (gated_few(p.M, p.F)) return launch_skinny_projections(p, GRAD, ACT, stream);
   switch (gated_tile(p.M, p.K, p.F)) {
     case TileKind::k256: return launch_tiles<Wide, GRAD, ACT>(p, stream);
     case TileKind::k128: return launch_tiles<Middle, GRAD, ACT>(p, stream);

@@ -125,7 +125,7 @@ struct Gated {
   long long lda, ldw, lddh, ldh, ldgu;
   int M, K, F;
 };
-// At most 32 rows (skinny.hip); grad: dgu in gu, as gated_kernel makes it.
+// As gated_few says (skinny.hip); grad: dgu in gu, as gated_kernel makes it.
 hipError_t launch_skinny_projections(const Gated& p, bool grad, Activation act, hipStream_t stream);
 hipError_t launch_gated_fwd(const Gated& p, Activation act, hipStream_t stream);
 size_t gated_bwd_workspace_bytes(int M, int K, int F);

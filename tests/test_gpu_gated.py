@@ -227,3 +227,11 @@ def test_the_pitch_of_a_single_row_counts_for_nothing():
         hx.helix_gated_linear_bwd(a, w, dh, da, dw, torch.empty(hx.helix_gated_linear_bwd_workspace_bytes(1, K, F), dtype=torch.uint8, device="cuda"), gu=gu)
         results.append((h, gu, da, dw))
     assert all(torch.equal(x, y) and y.abs().max() > 0 for x, y in zip(*results))
+
+
+# a wave's share of the contraction: none, less than what it has on its way, exactly that, twice that and some; token blocks whole and cut; neighbouring workgroups on either side of
+# the last group of sixteen; the widest that is left to the few-rows kernel and the narrowest that is not
+@pytest.mark.parametrize("M,K,F", [(1, 1536, 64), (4, 2048, 576), (15, 1664, 128), (16, 3200, 192), (17, 2944, 64), (32, 4736, 128), (29, 384, 1088), (16, 128, 8192), (3, 256, 8256), (32, 128, 8320)])
+def test_few_rows(M, K, F):
+    a, w, gu = _check_forward(M, K, F, "silu")
+    _check_backward(M, K, F, "silu", a, w, gu)
