@@ -1,13 +1,13 @@
 // The gated projections of at most 32 rows (tokens).
 //
-// The bytes of the weights are all that counts.  A compute unit has only so many lines on their way, about 450 whatever they are for (a column of workgroups takes 2.8 us for 1024
+// The bytes of the weights are all that counts.  A compute unit has only so many lines on their way, about 450 whatever asks for them (a workgroup takes 2.8 us for 1024
 // rows of w from the last cache, with 64 columns of both projections or 32, through LDS or into registers, with 96 or 256 KB asked for), so what helps is more compute units: a
 // workgroup has 32 columns of either projection, and neighbours, which share lines, are on one XCD.  Its waves share the contraction.  Each streams its own range of it straight into
 // registers, DEPTH groups of 32 rows of w ahead, and waits for nobody: a lane loads four columns of eight rows, which with the elements of two rows put side by side (one
 // byte permutation) are the contraction indices of four operands of the 16x16x32 MFMA.  An operand's 16 rows are every fourth column: the first eight of the gate, the
 // others the same columns of the other projection.  The partial sums are added up in LDS at the end, in a fixed order.
 //
-// One token, us (64 columns and stages in LDS / so, bytes): 2048 x 5504 11.5 / 10.2, 4.4 TB/s; 4096 x 4096 21.6 / 20.3; 1024 x 2752 7.1 / 5.9; 512 x 640 5.0 / 3.7.
+// One token, us (64 columns to a workgroup and stages in LDS / so): 2048 x 5504 11.5 / 10.2, 4.4 TB/s; 4096 x 4096 21.6 / 20.3; 1024 x 2752 7.1 / 5.9; 512 x 640 5.0 / 3.7.
 #include "gated_math.hpp"
 #include "helix_common.hpp"
 #include "kernels.hpp"
