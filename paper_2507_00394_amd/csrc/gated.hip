@@ -44,11 +44,10 @@ struct GatedBlocks {
   }
 };
 
-// A wave's part of dh, 32 * BI rows x 32 * BH columns, in registers: requested when the last copies are out, so that it is there when the sums are.  A lane loads
+// A wave's part of dh, 32 * BI rows x 32 * BH columns, in registers: requested when the last copies have landed, so that it is there when the sums are.  A lane loads
 // 16 bytes at a time of the row that its sums belong to, those of the lane 32 further on in between.
 template <int BI, int BH>
 struct Gradient {
-  static constexpr int IN_FLIGHT = BI * BH * 2;
   const __bf16* base;   // column of the wave's first block
   long long ld;
   int i_wave, M, lane;

@@ -212,9 +212,8 @@ struct BlocksSideBySide {
   __device__ __forceinline__ static constexpr int column(int BJ, int wj, int b) { return 32 * (BJ * wj + b); }
 };
 
-// What a wave asks of memory when the last copies of its stages are out: IN_FLIGHT loads that nothing waits for before the sums are complete.
+// What a wave asks of memory when the last copies of its stages have landed: loads that nothing waits for before the sums are complete.
 struct NothingBeforeTheEnd {
-  static constexpr int IN_FLIGHT = 0;
   __device__ __forceinline__ void operator()() const {}
 };
 
@@ -333,10 +332,22 @@ __device__ __forceinline__ void gemm_sums(XOp& xsrc, YOp& ysrc, int nk, uint32_t
     stage(std::true_type{}, std::true_type{});
     stage_barrier<(AHEAD - 2) * NDMA>();
   }
-  before_the_end();
-  for (; k < (STAGE_AHEAD ? nk - 1 : nk); k++) {
+  if constexpr (std::is_same<typename std::decay<Before>::type, NothingBeforeTheEnd>::value) {
+    for (; k < (STAGE_AHEAD ? nk - 1 : nk); k++) {
+      stage(std::false_type{}, std::true_type{});
+      stage_barrier<0>();
+    }
+  } else {
+    // The loads go out behind the barrier that has waited for the last copies, all of them, and the barriers after it wait for no memory: which copies have landed does not
+    // depend on how many load instructions the compiler makes or where it puts them.
+    static_assert(!STAGE_AHEAD, "the last stage is one of those below");
     stage(std::false_type{}, std::true_type{});
-    stage_barrier<std::remove_reference<Before>::type::IN_FLIGHT>();
+    stage_barrier<0>();
+    before_the_end();
+    for (k++; k < nk; k++) {
+      stage(std::false_type{}, std::true_type{});
+      asm volatile("s_barrier" ::: "memory");
+    }
   }
   // The last stage has nothing to read ahead and, as the tile leaves from the registers, nobody to wait for: its reads held up the workgroup beside this one (forward of
   // 12480 x 128 x 128 3.39 -> 3.27 us, 4256 x 512 x 256 4.91 -> 4.84).
