@@ -277,7 +277,8 @@ int helix_layer_norm_fwd(const void* x, long long ldx, const float* gamma, const
 int helix_layer_norm_bwd(const void* dy, long long lddy, const void* x, long long ldx, const float* gamma,
                          const float* mean, const float* rstd, void* dx, long long lddx, float* dgamma, float* dbeta,
                          void* workspace, size_t workspace_bytes, int M, int E, int type, void* stream);
-/* Bytes of scratch the two backward calls with a layer norm need (0 for an invalid shape).  Pure host arithmetic. */
+/* Bytes of scratch the two backward calls with a layer norm need (0 for an invalid shape), never fewer for more rows: a workspace for the largest M does
+ * for the smaller ones of the same E.  Pure host arithmetic. */
 size_t helix_layer_norm_bwd_workspace_bytes(int M, int E);
 
 /* Dropout, residual sum and layer norm in one pass, as they follow the output projection of attention:
@@ -314,7 +315,8 @@ int helix_gated_linear_fwd(const void* a, long long lda, const void* w, long lon
 int helix_gated_linear_bwd(const void* a, long long lda, const void* w, long long ldw, const void* gu, long long ldgu,
                            const void* dh, long long lddh, void* da, long long ldda, void* dw, long long lddw,
                            void* workspace, size_t workspace_bytes, int M, int K, int F, int activation, void* stream);
-/* Bytes of scratch helix_gated_linear_bwd needs (0 for an invalid shape).  Pure host arithmetic. */
+/* Bytes of scratch helix_gated_linear_bwd needs (0 for an invalid shape), never fewer for more tokens: a workspace for the largest M does for the smaller
+ * ones of the same K and F.  Pure host arithmetic. */
 size_t helix_gated_linear_bwd_workspace_bytes(int M, int K, int F);
 
 /* Whether `strides` (NULL: contiguous) is acceptable for a [B, H, S, D] view: HELIX_OK,

@@ -430,6 +430,7 @@ def helix_layer_norm_fwd(x, gamma, beta, y, mean, rstd, eps=1e-5, stream=None):
 
 
 def helix_layer_norm_bwd_workspace_bytes(M, E) -> int:
+    """Bytes for up to M rows of E columns."""
     return int(lib().helix_layer_norm_bwd_workspace_bytes(_length(M), _length(E)))
 
 
@@ -498,6 +499,7 @@ def helix_gated_linear_fwd(a, w, h, gu=None, activation="silu", stream=None):
 
 
 def helix_gated_linear_bwd_workspace_bytes(M, K, F) -> int:
+    """Bytes for up to M tokens."""
     return int(lib().helix_gated_linear_bwd_workspace_bytes(_length(M), _length(K), _length(F)))
 
 

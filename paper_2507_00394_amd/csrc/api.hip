@@ -369,7 +369,7 @@ int helix_dropout_add_layer_norm_fwd(const void* x, long long ldx, const void* r
 
 size_t helix_layer_norm_bwd_workspace_bytes(int M, int E) {
   if (M < 1 || E < 1 || E > HELIX_NORM_MAX_COLS) return 0;
-  return ((size_t)helix::norm_bwd_groups(M, E) * 2 * E * sizeof(float) + 255) & ~(size_t)255;
+  return ((size_t)helix::norm_bwd_slabs(M, E) * 2 * E * sizeof(float) + 255) & ~(size_t)255;
 }
 
 int helix_layer_norm_bwd(const void* dy, long long lddy, const void* x, long long ldx, const float* gamma,

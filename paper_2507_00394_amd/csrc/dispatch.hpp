@@ -338,12 +338,22 @@ inline TilePair linear_gradient_tiles(int M, int K, int N, int parts) {
 // Whole / in parts, us of the backward from kept projections, M x K x F: 1 x 2048 x 5504 60 / 31; 1 x 4096 x 11008 149 / 110; 32 x 1024 x 8192 52 / 31; 300 x 4096 x 4096
 // 120 / 87; 700 x 2048 x 5504 172 / 128; 700 x 512 x 9984 117 / 78; 2000 x 1024 x 5504 184 / 144; 4000 x 512 x 8000 290 / 238; 6000 x 640 x 9984 517 / 516; 8000 x 512 x
 // 5504 340 / 357; 8 x 5120 x 1728 21 / 27; 100 x 1024 x 2752 22.9 / 24.6; 300 x 1024 x 1024 13 / 21.
+constexpr int kSplitInputRows = 4096;
 inline TileKind split_input_tile(int M) { return M <= 64 ? TileKind::k64 : TileKind::k128; }
 inline int split_input_parts(int M, int K, int N) {
   const int e = tile_edge(split_input_tile(M));
   const long long tiles = (long long)((M + e - 1) / e) * ((K + e - 1) / e);
-  if (M > 4096 || N < 6144 || tiles >= 512) return 1;
+  if (M > kSplitInputRows || N < 6144 || tiles >= 512) return 1;
   return (int)std::min<long long>(std::min<long long>((512 + tiles - 1) / tiles, N / 256), 32);
+}
+// Rows of partial sums, parts x M, that a workspace for M rows has room for: the most that M rows or fewer need, as fewer rows can have more parts.  Only whole tiles have to be looked at.
+inline long long split_input_rows(int M, int K, int N) {
+  long long most = 0;
+  for (int m = std::min(M, kSplitInputRows); m > 0; m = m > 64 ? (m > 128 ? (m - 1) / 128 * 128 : 64) : 0) {
+    const int parts = split_input_parts(m, K, N);
+    if (parts > 1) most = std::max(most, (long long)parts * m);
+  }
+  return most;
 }
 
 // Its weight gradient: parts until the 256 x 256 tiles fill half of the chip; the input gradient's workgroups, which share the launch, fill the rest, and every part less is a
@@ -417,5 +427,8 @@ inline int norm_bwd_groups(int rows, int cols) {
   const long long turns = ((long long)rows + together - 1) / together;
   return turns <= 2 ? 1 : (int)std::min<long long>(turns, 256);
 }
+// Slabs that a workspace for so many rows has room for: the most that as many rows or fewer leave.  There are 256 as soon as each of 256 workgroups has a single wave's rows; with more
+// rows it may have more at a time and the chip fewer workgroups.
+inline int norm_bwd_slabs(int rows, int cols) { return norm_bwd_groups(std::min(rows, norm_bwd_rows(cols) == NormBwdRows::k16x2 ? 4 * 256 : 256), cols); }
 
 }  // namespace helix

@@ -112,10 +112,10 @@ size_t linear_bwd_workspace_bytes(int M, int K, int N) {
   return linear_bwd_wt_bytes(K, N) + (parts > 1 ? (size_t)parts * K * N * sizeof(float) : 0);
 }
 
-// With the input gradient in parts (linear_bwd with RAGGED only): the slabs hold either's partial results.
+// With the input gradient in parts (linear_bwd with RAGGED only): the slabs hold either's partial results.  No less than fewer rows need.
 size_t linear_bwd_ragged_workspace_bytes(int M, int K, int N) {
-  const int parts = split_weight_parts(M, K, N), input_parts = split_input_parts(M, K, N);
-  return linear_bwd_wt_bytes(K, N) + std::max(parts > 1 ? (size_t)parts * K * N * sizeof(float) : 0, input_parts > 1 ? (size_t)input_parts * M * K * sizeof(float) : 0);
+  const int parts = split_weight_parts(M, K, N);
+  return linear_bwd_wt_bytes(K, N) + std::max(parts > 1 ? (size_t)parts * K * N * sizeof(float) : 0, (size_t)split_input_rows(M, K, N) * K * sizeof(float));
 }
 
 // Input gradient da = dout * w^T.  With w as stored ([K][N], contraction index n contiguous) both
