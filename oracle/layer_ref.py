@@ -74,9 +74,9 @@ def activation_ref(g, kind):
     if kind == "silu":
         s = 0.5 * (1 + np.tanh(0.5 * g))
         return g * s, s + g * s * (1 - s)
-    from scipy.special import erf
+    from scipy.special import erfc
 
-    P = 0.5 * (1 + erf(g / np.sqrt(2)))
+    P = 0.5 * erfc(-g / np.sqrt(2))   # 1 + erf has no correct digit left below -8
     return g * P, P + g * np.exp(-g * g / 2) / np.sqrt(2 * np.pi)
 
 
