@@ -21,6 +21,8 @@ static __device__ __align__(256) unsigned char scratch[kScratchBytes];
 
 constexpr int kVersion = 400;  // 0.4.0: the row-wise operators around the attention stage
 
+static_assert(HELIX_NORM_MAX_COLS == helix::kNormMaxCols, "rows that the widest variant holds");
+
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 
 int check_shape(int B, int H, int S, int D) {

@@ -393,12 +393,11 @@ inline TileKind gated_tile(int M, int K, int F) {
 //
 // How many lanes hold a row, and how many chunks of 8 columns a lane at most: as few lanes as have it in registers, with few registers a lane.
 enum class NormRows { k16x2, k64x2, k256x1, k256x2, k512x2, k1024x2 };
-constexpr int kNormMaxCols = 16384;
+constexpr int kNormMaxCols = 1024 * 2 * 8;   // k1024x2
 inline NormRows norm_rows(int cols) {
   return cols <= 256 ? NormRows::k16x2 : cols <= 1024 ? NormRows::k64x2 : cols <= 2048 ? NormRows::k256x1 : cols <= 4096 ? NormRows::k256x2
        : cols <= 8192 ? NormRows::k512x2 : NormRows::k1024x2;
 }
-inline int norm_lanes(NormRows r) { return r == NormRows::k16x2 ? 16 : r == NormRows::k64x2 ? 64 : r == NormRows::k512x2 ? 512 : r == NormRows::k1024x2 ? 1024 : 256; }
 // Waves of the forward kernel on a SIMD; its registers are limited to what so many leave.  SUM: with dropout and residual sum.  Beyond what keeps the memory
 // busy more of them change little (us with 7 / 5 / 4, SUM 5 / 4 / 3 / 2: layer norm of 131072 x 4096 400 / 386 / 400, 8192 x 5001 34 / 41 / 41, SUM 32768 x 4096 201 /
 // 192 / 190 / 225, 20000 x 900 27.3 / 27.3 / 28.4 / 31.9).
