@@ -391,22 +391,28 @@ inline TileKind gated_tile(int M, int K, int F) {
 
 // ---------------------------------------------------------------- layer norm's rows
 //
-// How many lanes hold a row, and how many chunks of 8 columns a lane at most: as few lanes as have it in registers, with few registers a lane.
+// How many lanes hold a row, and how many chunks of 8 columns a lane at most: as few lanes as have it in registers, with few registers a lane.  At the limits, us for 2^26 elements of bf16 so /
+// with the next variant: 256 columns 49 / 65, 1024 49 / 58, 2048 49 / 49, 4096 50 / 50, 8192 48 / 65; with dropout and sum 94 / 153, 94 / 117, 95 / 104, 94 / 104, 92 / 107.  fp32: 103 / 124,
+// 103 / 105, 104 / 105, 101 / 101, 102 / 112; 204 / 231, 202 / 215, 208 / 206, 201 / 198, 200 / 196.
 enum class NormRows { k16x2, k64x2, k256x1, k256x2, k512x2, k1024x2 };
 constexpr int kNormMaxCols = 1024 * 2 * 8;   // k1024x2
 inline NormRows norm_rows(int cols) {
   return cols <= 256 ? NormRows::k16x2 : cols <= 1024 ? NormRows::k64x2 : cols <= 2048 ? NormRows::k256x1 : cols <= 4096 ? NormRows::k256x2
        : cols <= 8192 ? NormRows::k512x2 : NormRows::k1024x2;
 }
-// Waves of the forward kernel on a SIMD; its registers are limited to what so many leave.  SUM: with dropout and residual sum.  Beyond what keeps the memory
-// busy more of them change little (us with 7 / 5 / 4, SUM 5 / 4 / 3 / 2: layer norm of 131072 x 4096 400 / 386 / 400, 8192 x 5001 34 / 41 / 41, SUM 32768 x 4096 201 /
-// 192 / 190 / 225, 20000 x 900 27.3 / 27.3 / 28.4 / 31.9).
-constexpr int norm_fwd_waves(int L, int NC, bool sum) { return L == 1024 ? 4 : sum ? (NC == 2 ? 4 : 7) : NC == 2 ? 7 : 8; }
+// Waves of the forward kernel on a SIMD: as many as its registers allow; more would put some of them into memory.  (1024 lanes are a whole workgroup of 16 waves.)  Beyond what keeps the memory busy
+// more of them change little, and what they change goes either way with the width.  us with 8 / 7 / 6 / 5 / 4 waves, one chunk: 20000 x 1500 23.1 / 24.0 / 24.9 / 26.2 / 29.9, 131072 x 2048 194 /
+// 196 / 199 / 196 / 199; with dropout and sum 54.9 / 58.2 / 63.5 / 69.0 / 78.6, 388 / 396 / 403 / 396 / 406.  Two chunks, 7 / 6 / 5 / 4: 131072 x 4096 400 / 402 / 383 / 410, 30000 x 3000 66.7 / 67.8 /
+// 72.5 / 82.7, 8192 x 5001 34.7 / 34.7 / 41.2 / 42.2, 32768 x 8192 189 / 184 / 196 / 195; with dropout and sum, 4 / 3 / 2: 131072 x 4096 823 / 803 / 881, 30000 x 3000 139 / 154 / 201, 8192 x 5001 93.8 /
+// 133 / 134, 32768 x 8192 377 / 448 / 447.
+constexpr int norm_fwd_waves(int L, int NC, bool sum) { return L == 1024 ? 4 : NC == 1 ? 8 : sum ? 4 : 7; }
 // Workgroups of `threads` that the chip holds at once with so many waves on a SIMD.  More would run when the others have ended, with the chip nearly empty.
 constexpr int groups_at_once(int threads, int waves) { return 256 * (waves * 256 / threads); }
 
 // The gradient: one workgroup to a compute unit, of as many threads as there can be, so of several rows at a time; with few rows
-// of fewer, so that all compute units have some.
+// of fewer, so that all compute units have some.  At the limits, us for 2^26 elements of bf16 so / with the next variant: 256 columns 81 / 109, 1024 81 / 86, 2048 79 / 86, 4096 80 / 88,
+// 8192 84 / 92; with dropout and sum 130 / 221, 130 / 142, 125 / 142, 131 / 143, 131 / 148.  fp32: 159 / 159, 159 / 148, 158 / 147, 159 / 148, 163 / 154; 266 / 276, 266 / 246, 257 / 245, 263 / 247,
+// 261 / 249: one rule for all types, which leaves fp32 5 to 7 % behind near a limit.
 enum class NormBwdRows { k16x2, k64x2, k128x2, k256x2, k512x2, k1024x2 };
 inline NormBwdRows norm_bwd_rows(int cols) {
   return cols <= 256 ? NormBwdRows::k16x2 : cols <= 1024 ? NormBwdRows::k64x2 : cols <= 2048 ? NormBwdRows::k128x2 : cols <= 4096 ? NormBwdRows::k256x2
