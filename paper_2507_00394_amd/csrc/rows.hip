@@ -344,7 +344,7 @@ __global__ void __launch_bounds__(kNormBwdThreads) layer_norm_bwd_kernel(NormBwd
     int lane = at.l;
     pin(lane);   // gamma is read here, not once for all rows into registers
     if (at.tail) {
-      xt = (at.load_tail(x) - mean) * rstd;
+      xt = at.has_tail ? (at.load_tail(x) - mean) * rstd : 0.f;
       gt = at.load_tail(dy);
       dgamma_tail = fmaf(gt, xt, dgamma_tail);
       dbeta_tail += gt;
@@ -354,10 +354,11 @@ __global__ void __launch_bounds__(kNormBwdThreads) layer_norm_bwd_kernel(NormBwd
     }
 #pragma unroll
     for (int i = 0; i < NC; i++) {
-      const f32x8 d = widen(gc[i]), xh = (widen(xc[i]) - mean) * rstd, gamma = gamma_of(i, lane);
+      // in columns that do not exist dy, gamma and xh are zero: mean * rstd may leave the range of fp32 where no x - mean does
+      const f32x8 d = widen(gc[i]), xh = (widen(xc[i]) - (at.has[i] ? mean : 0.f)) * rstd, gamma = gamma_of(i, lane);
       dbeta[i] += d;
 #pragma unroll
-      for (int e = 0; e < 8; e++) {   // dy and gamma are zero in columns that do not exist
+      for (int e = 0; e < 8; e++) {
         dgamma[i][e] = fmaf(d[e], xh[e], dgamma[i][e]);
         const float g = d[e] * gamma[e];
         sums[0] += g;
