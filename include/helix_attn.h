@@ -308,7 +308,7 @@ int helix_dropout_add_layer_norm_bwd(const void* dy, long long lddy, const void*
  * ld* as for helix_qkv_linear_fwd: 16-byte aligned, ld* at least the row length, a multiple of 8, at most 2^22 (HELIX_ERR_BAD_STRIDE).
  * The down projection h -> [M][K] is helix_qkv_linear_fwd / _bwd with F, then a multiple of 128, in the place of K.
  * workspace: device memory of at least helix_gated_linear_bwd_workspace_bytes(M, K, F) bytes, 256-byte aligned, contents undefined
- * afterwards: [dg du], and what helix_qkv_linear_bwd keeps there.  No atomics: every bit is reproduced.  M, K and F decide which
+ * afterwards: [dg du], what helix_qkv_linear_bwd keeps there, and partial sums of da where its contraction is long.  No atomics: every bit is reproduced.  M, K and F decide which
  * tiles a call takes and with them the order of its sums: a token's results in calls of different M agree within rounding. */
 int helix_gated_linear_fwd(const void* a, long long lda, const void* w, long long ldw, void* gu, long long ldgu,
                            void* h, long long ldh, int M, int K, int F, int activation, void* stream);
